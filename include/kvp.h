@@ -366,6 +366,79 @@ int kvp_probe_copy(void* device_dst, const void* device_src, size_t bytes, int32
 
 void kvp_free_cache(kvp_cache* cache);   /* host object only; NULL is fine */
 
+/* ---- Many sequences at once --------------------------------------------------
+ *
+ * What kvp_cache is for one long prefix, pages are for the keys and values of many
+ * sequences: of requests whose prompts need no compression (kvp_prompt_attention),
+ * and of compressed caches between or after their prefills.  These calls have no
+ * host object and no state; everything they are told comes through their arguments.
+ * The general rules above hold.  Sequences and their lengths are DEVICE data (an
+ * int32 each), so that a captured graph or a loop that does not wait can go on with
+ * other lengths, and nothing can be refused for what they hold: a number out of its
+ * range is brought into it as each call says, and nothing outside the caller's
+ * tensors is read or written for it.
+ *
+ * Device tensors of bf16 numbers start at a multiple of 16 bytes; strides are in
+ * elements, multiples of 8 and not negative, those from token to token below 2^23 and
+ * those from head to head below 2^40.  Rows of a tensor that is written do not overlap.
+ * All device tensors are on the device of `stream`, which is the current one. */
+
+enum { KVP_PAGE_BF16 = 0, KVP_PAGE_E4M3 = 1 };
+enum {
+  KVP_MAX_SEQUENCES = 4096,         /* per call                                        */
+  KVP_MAX_PAGE_SIZE = 256
+};
+
+/* Pages of one layer.  Token p of a sequence lies in row p % page_size of the page
+ * with number table[sequence][p / page_size].  With KVP_PAGE_E4M3 a row of
+ * head_dim numbers x is held as 8-bit numbers y (e4m3: 4 bits of exponent, 3 behind
+ * the point, no infinities) and one byte e + 127, x = y 2^e, where e is the least
+ * number from -126 on for which the largest finite magnitude of the row is at most
+ * 448 2^e.  Numbers are rounded to the nearest y, ties to the even one; one that is
+ * not finite becomes a NaN.  Every x that is held for a bf16 number is a bf16 number
+ * again, but for 2^128, which 1.9375 * 2^127 and more round to: read back, an infinity. */
+typedef struct kvp_pages {
+  void* k;              /* device [n_pages, n_kv_heads, page_size, head_dim] */
+  void* v;              /* the same                                        */
+  void* k_exp;          /* device [n_pages, n_kv_heads, page_size] uint8, 4-byte aligned; */
+  void* v_exp;          /* both NULL for KVP_PAGE_BF16                        */
+  int32_t format;       /* KVP_PAGE_*                                       */
+  int32_t n_pages;      /* n_pages * page_size * n_kv_heads < 2^40           */
+  int32_t n_kv_heads;
+  int32_t page_size;    /* 16, 32, 64, 128 or 256                            */
+  int32_t head_dim;     /* 64 or 128                                        */
+} kvp_pages;
+
+/* Keys and values of n_tokens tokens, bf16: number c of head h of token t is at
+ * t * token + h * head + c.  A projection's rows [n_tokens, n_kv_heads, head_dim] have
+ * strides n_kv_heads * head_dim and head_dim, a kvp_view's head_dim and budget * head_dim. */
+typedef struct kvp_rows {
+  void* k;
+  void* v;
+  int64_t k_token, k_head;
+  int64_t v_token, v_head;
+  int32_t n_tokens;     /* n_tokens * n_kv_heads < 2^31                      */
+} kvp_rows;
+
+/* Writes tokens into the pages of their sequences.  Tokens seq_begin[s] ..
+ * seq_begin[s + 1] - 1 of `rows` become tokens first[s], first[s] + 1, ... of
+ * sequence s (first NULL: from 0 on).
+ *   seq_begin  device [n_seqs + 1], not descending from 0 on
+ *   table      device [n_seqs, table_width], page numbers; table_width * page_size <= 2^30
+ *   first      device [n_seqs], or NULL
+ * A token is left out that has no sequence (before seq_begin[0], or from
+ * seq_begin[n_seqs] on), whose place lies outside the table, or whose page number is
+ * not in 0 .. n_pages - 1.  Of tokens with the same place in the pages each number is
+ * left by one of them.  Nothing else in the pages is touched.  n_tokens = 0 does nothing. */
+int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
+                   int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream);
+
+/* The way back, exactly: the tokens that kvp_page_write with the same arguments would
+ * have written are read from the pages into `rows`.  Tokens that it would have left
+ * out become zeros, but those that have no sequence are left as they were. */
+int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
+                  int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

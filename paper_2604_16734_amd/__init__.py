@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     kvp_decode_ready, kvp_set_state, kvp_set_attention_shape, kvp_set_score_sweep, kvp_debug_last,
     kvp_profile_enable,
     kvp_profile_read, kvp_kernel_name, kvp_debug_totals, TOTALS, kvp_probe_mfma, kvp_probe_copy, kvp_free_cache,
-    Cache,
+    Cache, KVP_PAGE_BF16, KVP_PAGE_E4M3, KVP_MAX_SEQUENCES, KVP_MAX_PAGE_SIZE, KvpPages, KvpRows, kvp_page_write, kvp_page_read,
 )
+from .pages import Pages  # noqa: F401
 from .runtime import Prefill, LayerwisePrefill  # noqa: F401

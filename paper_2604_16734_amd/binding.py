@@ -42,6 +42,20 @@ class KvpView(ctypes.Structure):
                 ("next_token", ctypes.c_int32)]
 
 
+KVP_PAGE_BF16, KVP_PAGE_E4M3 = 0, 1
+KVP_MAX_SEQUENCES, KVP_MAX_PAGE_SIZE = 4096, 256
+
+
+class KvpPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
+               [(n, ctypes.c_int32) for n in ("format", "n_pages", "n_kv_heads", "page_size", "head_dim")]
+
+
+class KvpRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("k_token", "k_head", "v_token", "v_head")] + [("n_tokens", ctypes.c_int32)]
+
+
 class KvpKernelStat(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("layers", ctypes.c_int64), ("total_ms", ctypes.c_double)]
 
@@ -121,6 +135,9 @@ def lib():
         L.kvp_probe_mfma.argtypes = [vp, sz, i32, i32, vp, P(ctypes.c_double)]
         L.kvp_probe_copy.restype = ctypes.c_int
         L.kvp_probe_copy.argtypes = [vp, vp, sz, i32, vp]
+        for name in ("kvp_page_write", "kvp_page_read"):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = [P(KvpPages), P(KvpRows), vp, vp, i32, vp, i32, vp]
         L.kvp_free_cache.restype = None
         L.kvp_free_cache.argtypes = [vp]
         _lib = L
@@ -305,6 +322,14 @@ def kvp_probe_mfma(device_out, out_bytes, workgroups, iters, stream=0):
 
 def kvp_probe_copy(device_dst, device_src, nbytes, workgroups, stream=0):
     return lib().kvp_probe_copy(device_dst, device_src, nbytes, workgroups, stream)
+
+
+def kvp_page_write(pages, rows, seq_begin, table, table_width, first, n_seqs, stream=0):
+    return lib().kvp_page_write(ctypes.byref(pages), ctypes.byref(rows), seq_begin, table, table_width, first, n_seqs, stream)
+
+
+def kvp_page_read(pages, rows, seq_begin, table, table_width, first, n_seqs, stream=0):
+    return lib().kvp_page_read(ctypes.byref(pages), ctypes.byref(rows), seq_begin, table, table_width, first, n_seqs, stream)
 
 
 def kvp_free_cache(handle):

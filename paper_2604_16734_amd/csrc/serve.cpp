@@ -1,0 +1,87 @@
+// Host side of the calls that serve many sequences at once: checks of the arguments and launches.  No state; no device memory is
+// allocated and no stream is synchronised.
+#include <cmath>
+
+#include "serve.h"
+
+using namespace kvp;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t to) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+bool valid_pages(const kvp_pages* p) {
+  if (!p || (p->format != KVP_PAGE_BF16 && p->format != KVP_PAGE_E4M3)) return false;
+  if (p->head_dim != 64 && p->head_dim != 128) return false;
+  if (p->page_size < 16 || p->page_size > KVP_MAX_PAGE_SIZE || (p->page_size & (p->page_size - 1)) != 0) return false;
+  if (p->n_pages < 1 || p->n_kv_heads < 1) return false;
+  if ((unsigned long long)p->n_pages * (unsigned)p->n_kv_heads >= (1ull << 40) / (unsigned)p->page_size) return false;
+  if (!aligned(p->k, 16) || !aligned(p->v, 16)) return false;
+  if (p->format == KVP_PAGE_E4M3) return aligned(p->k_exp, 4) && aligned(p->v_exp, 4);
+  return !p->k_exp && !p->v_exp;
+}
+
+Pool pool_of(const kvp_pages& p) {
+  int shift = 4;
+  while ((1 << shift) < p.page_size) ++shift;
+  return Pool{static_cast<char*>(p.k), static_cast<char*>(p.v), static_cast<uint8_t*>(p.k_exp), static_cast<uint8_t*>(p.v_exp),
+              p.n_pages, p.n_kv_heads, shift};
+}
+
+bool valid_strides(int64_t token, int64_t head) {
+  return token >= 0 && token < (1 << 23) && token % 8 == 0 && head >= 0 && head < (1ll << 40) && head % 8 == 0;
+}
+// [n_tokens, n_heads, dim] rows that do not overlap: the rows of a token inside the distance of two tokens, or the other way round
+bool separate_rows(int64_t token, int64_t head, int n_tokens, int n_heads, int dim) {
+  if ((n_tokens > 1 && token < dim) || (n_heads > 1 && head < dim)) return false;
+  if (n_tokens <= 1 || n_heads <= 1) return true;
+  return token >= (n_heads - 1) * head + dim || head >= (n_tokens - 1) * token + dim;
+}
+
+bool valid_table(const int32_t* table, int32_t width, int32_t page_size, int32_t n_seqs) {
+  return aligned(table, 4) && width >= 1 && width <= (1 << 30) / page_size && n_seqs >= 1 && n_seqs <= KVP_MAX_SEQUENCES;
+}
+
+int code_of(hipError_t e) { return e == hipSuccess ? KVP_OK : KVP_EDEVICE; }
+
+int page_rows(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table, int32_t width,
+              const int32_t* first, int32_t n_seqs, void* stream, bool write) {
+  if (!valid_pages(pages) || !rows || !valid_table(table, width, pages->page_size, n_seqs)) return KVP_EINVAL;
+  if (!aligned(seq_begin, 4) || (first && !aligned(first, 4))) return KVP_EINVAL;
+  if (rows->n_tokens < 0 || (long long)rows->n_tokens * pages->n_kv_heads >= 1ll << 31) return KVP_EINVAL;
+  if (!valid_strides(rows->k_token, rows->k_head) || !valid_strides(rows->v_token, rows->v_head)) return KVP_EINVAL;
+  if (!write && (!separate_rows(rows->k_token, rows->k_head, rows->n_tokens, pages->n_kv_heads, pages->head_dim) ||
+                 !separate_rows(rows->v_token, rows->v_head, rows->n_tokens, pages->n_kv_heads, pages->head_dim)))
+    return KVP_EINVAL;
+  if (rows->n_tokens == 0) return KVP_OK;
+  if (!aligned(rows->k, 16) || !aligned(rows->v, 16)) return KVP_EINVAL;
+  PageRowsArgs a{};
+  a.pool = pool_of(*pages);
+  a.k = static_cast<u16*>(rows->k);
+  a.v = static_cast<u16*>(rows->v);
+  a.k_token = rows->k_token; a.k_head = rows->k_head;
+  a.v_token = rows->v_token; a.v_head = rows->v_head;
+  a.seq_begin = seq_begin; a.table = table; a.first = first;
+  a.width = width; a.n_seqs = n_seqs;
+  a.n_rows = rows->n_tokens * pages->n_kv_heads;
+  a.by_heads = divisor_of((unsigned)pages->n_kv_heads, (unsigned)a.n_rows);
+  const bool e4m3 = pages->format == KVP_PAGE_E4M3;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return code_of(write ? launch_page_write(a, pages->head_dim, e4m3, s) : launch_page_read(a, pages->head_dim, e4m3, s));
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
+                   int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream) {
+  return page_rows(pages, rows, seq_begin, table, table_width, first, n_seqs, stream, true);
+}
+
+int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
+                  int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream) {
+  return page_rows(pages, rows, seq_begin, table, table_width, first, n_seqs, stream, false);
+}
+
+}  // extern "C"

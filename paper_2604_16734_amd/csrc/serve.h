@@ -1,0 +1,32 @@
+// Arguments of the kernels that serve many sequences at once (serve.cpp checks them, pages.hip, paged_decode.hip and prompt.hip run them).
+#pragma once
+#include "kvp_internal.h"
+#include "pages.h"
+
+namespace kvp {
+
+struct Pool {
+  char* k;                    // [n_pages][n_heads][page size][head_dim], bf16 or e4m3
+  char* v;
+  uint8_t* k_exp;             // [n_pages][n_heads][page size], e4m3 only
+  uint8_t* v_exp;
+  int n_pages, n_heads, shift;
+};
+
+struct PageRowsArgs {
+  Pool pool;
+  u16* k;                     // the rows outside the pages
+  u16* v;
+  long long k_token, k_head, v_token, v_head;
+  const int32_t* seq_begin;
+  const int32_t* table;
+  const int32_t* first;       // or null
+  int width, n_seqs;
+  int n_rows;                 // tokens * heads, heads fastest
+  Divisor by_heads;
+};
+
+hipError_t launch_page_write(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
+hipError_t launch_page_read(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
+
+}  // namespace kvp

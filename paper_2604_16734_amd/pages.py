@@ -1,0 +1,115 @@
+"""Keys and values of many sequences in pages: a holder of the tensors, and the calls of include/kvp.h that serve many sequences at
+once with torch tensors as their arguments.  Marshalling only, as in binding.py."""
+import contextlib
+import ctypes
+
+from .binding import (KVP_EINVAL, KVP_PAGE_BF16, KVP_PAGE_E4M3, KvpError, KvpPages, KvpRows, lib)
+
+
+def _need(ok, what):
+    if not ok:
+        raise KvpError(KVP_EINVAL, what)
+
+
+class _On:
+    """The device and stream of a call: torch's current stream of the tensors' device, or the caller's."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.index = device.index
+        self.handle = torch._C._cuda_getCurrentRawStream(self.index)
+        self.others = None
+        if stream is not None:
+            handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+            if handle != self.handle:
+                self.handle, self.others = handle, torch.cuda.ExternalStream(handle, device=device)
+        self.away = torch._C._cuda_getDevice() != self.index
+
+    def __enter__(self):
+        """What is allocated inside belongs to the call's stream."""
+        import torch
+        self.stack = None
+        if self.away or self.others is not None:
+            self.stack = contextlib.ExitStack()
+            if self.away:
+                self.stack.enter_context(torch.cuda.device(self.index))
+            if self.others is not None:
+                self.stack.enter_context(torch.cuda.stream(self.others))
+        return self.handle
+
+    def __exit__(self, *of):
+        if self.stack is not None:
+            self.stack.__exit__(*of)
+
+
+def _numbers(t, shape, device, what):
+    """(address, token stride, head stride) of bf16 rows [tokens, heads, d]."""
+    import torch
+    _need(t.dtype is torch.bfloat16 and t.device == device and t.shape == shape, what)
+    token, head, one = t.stride()
+    _need(one == 1, what)
+    return t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def _whole(t, shape, device, what):
+    """Address of contiguous int32 numbers."""
+    import torch
+    _need(t.dtype is torch.int32 and t.device == device and t.shape == shape and t.is_contiguous(), what)
+    return t.data_ptr()
+
+
+class Pages:
+    """Pages of one layer over the caller's tensors, [n_pages, n_kv_heads, page_size, head_dim]: `k` and `v` of bf16, or of e4m3
+    (torch.float8_e4m3fn) with exponents `k_exp` and `v_exp`, uint8 [n_pages, n_kv_heads, page_size]."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        import torch
+        e4m3 = k.dtype is torch.float8_e4m3fn
+        _need(k.dim() == 4 and (e4m3 or k.dtype is torch.bfloat16), "Pages: k")
+        _need(v.shape == k.shape and v.dtype is k.dtype and v.device == k.device, "Pages: v")
+        _need(k.is_contiguous() and v.is_contiguous(), "Pages: contiguous k and v")
+        _need(k.device.type == "cuda" and k.device.index is not None, "Pages: on a GPU")
+        for t in (k_exp, v_exp):
+            _need((t is not None) == e4m3, "Pages: exponents belong to e4m3")
+            if t is not None:
+                _need(t.shape == k.shape[:3] and t.dtype is torch.uint8 and t.device == k.device and t.is_contiguous(), "Pages: exponents")
+        self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.of = KvpPages(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if e4m3 else None, v_exp.data_ptr() if e4m3 else None,
+                           KVP_PAGE_E4M3 if e4m3 else KVP_PAGE_BF16, *k.shape)
+        self._ref, self._lib = ctypes.byref(self.of), lib()
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, page_size=64, e4m3=False, device="cuda:0"):
+        """New tensors, not filled."""
+        import torch
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+        if not e4m3:
+            return cls(new(shape, torch.bfloat16), new(shape, torch.bfloat16))
+        return cls(new(shape, torch.float8_e4m3fn), new(shape, torch.float8_e4m3fn), new(shape[:3], torch.uint8), new(shape[:3], torch.uint8))
+
+    def _rows(self, call, k, v, seq_begin, table, first, stream):
+        n_tokens, n_seqs, device = k.shape[0], seq_begin.numel() - 1, self.device
+        what = "Pages.%s: " % call
+        shape = (n_tokens, self.n_kv_heads, self.head_dim)
+        k_at, k_token, k_head = _numbers(k, shape, device, what + "k")
+        v_at, v_token, v_head = _numbers(v, shape, device, what + "v")
+        _need(table.dim() == 2, what + "table")
+        rows = KvpRows(k_at, v_at, k_token, k_head, v_token, v_head, n_tokens)
+        args = (self._ref, ctypes.byref(rows), _whole(seq_begin, (n_seqs + 1,), device, what + "seq_begin"),
+                _whole(table, (n_seqs, table.shape[1]), device, what + "table"), table.shape[1],
+                None if first is None else _whole(first, (n_seqs,), device, what + "first"), n_seqs)
+        with _On(device, stream) as handle:
+            rc = getattr(self._lib, "kvp_page_" + call)(*args, handle)
+        if rc:
+            raise KvpError(rc, "kvp_page_" + call)
+
+    def write(self, k, v, seq_begin, table, first=None, stream=None):
+        """Rows seq_begin[s] .. seq_begin[s + 1] - 1 of k and v [n_tokens, n_kv_heads, head_dim] (any strides but the last) become
+        tokens first[s], first[s] + 1, ... of sequence s, whose pages are table[s] (kvp_page_write)."""
+        self._rows("write", k, v, seq_begin, table, first, stream)
+
+    def read(self, k, v, seq_begin, table, first=None, stream=None):
+        """The way back, into k and v (kvp_page_read)."""
+        self._rows("read", k, v, seq_begin, table, first, stream)
