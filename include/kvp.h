@@ -439,6 +439,28 @@ int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* 
 int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
                   int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream);
 
+/* One decode step of one layer for many sequences, each over its own pages (Eq. 1
+ * with one query row per head, as kvp_decode_step):
+ *   q          bf16, number c of head h of sequence s at s * q_token + h * q_head + c
+ *   lengths    device [n_seqs]: the keys of sequence s are its tokens 0 .. lengths[s] - 1,
+ *              the current one among them; brought into 0 .. table_width * page_size
+ *   out        [n_seqs, n_q_heads, head_dim] bf16, contiguous
+ *   workspace  device, 16-byte aligned, at least kvp_paged_decode_bytes(pages, n_q_heads).
+ *              Needs no clearing and keeps nothing from call to call; calls that may
+ *              overlap in time need one each.
+ * out[s, h] = softmax(scale * q[s, h] . K^T) V over the keys of KV head
+ * h / (n_q_heads / n_kv_heads), in fp32, rounded once; softmax_scale 0 means
+ * 1/sqrt(head_dim).  Keys of a page whose number is not in 0 .. n_pages - 1 take no
+ * part, whatever the pages hold behind a sequence's end neither; a sequence that is
+ * left with no key has zeros for its result.  The same arguments give the same bits.
+ * KVP_EINVAL also for more than 16 query heads per KV head, and where
+ * n_seqs * n_kv_heads * table_width * page_size passes 2^38; KVP_ENOMEM for a
+ * workspace that is too small. */
+size_t kvp_paged_decode_bytes(const kvp_pages* pages, int32_t n_q_heads);
+int kvp_paged_decode(const kvp_pages* pages, const void* q, int64_t q_token, int64_t q_head, int32_t n_q_heads,
+                     const int32_t* table, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
+                     float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

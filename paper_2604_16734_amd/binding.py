@@ -138,6 +138,10 @@ def lib():
         for name in ("kvp_page_write", "kvp_page_read"):
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = [P(KvpPages), P(KvpRows), vp, vp, i32, vp, i32, vp]
+        L.kvp_paged_decode_bytes.restype = sz
+        L.kvp_paged_decode_bytes.argtypes = [P(KvpPages), i32]
+        L.kvp_paged_decode.restype = ctypes.c_int
+        L.kvp_paged_decode.argtypes = [P(KvpPages), vp, ctypes.c_int64, ctypes.c_int64, i32, vp, i32, vp, i32, ctypes.c_float, vp, vp, sz, vp]
         L.kvp_free_cache.restype = None
         L.kvp_free_cache.argtypes = [vp]
         _lib = L
@@ -330,6 +334,16 @@ def kvp_page_write(pages, rows, seq_begin, table, table_width, first, n_seqs, st
 
 def kvp_page_read(pages, rows, seq_begin, table, table_width, first, n_seqs, stream=0):
     return lib().kvp_page_read(ctypes.byref(pages), ctypes.byref(rows), seq_begin, table, table_width, first, n_seqs, stream)
+
+
+def kvp_paged_decode_bytes(pages, n_q_heads):
+    return lib().kvp_paged_decode_bytes(ctypes.byref(pages), n_q_heads)
+
+
+def kvp_paged_decode(pages, q, q_token, q_head, n_q_heads, table, table_width, lengths, n_seqs, softmax_scale, out, workspace,
+                     workspace_bytes, stream=0):
+    return lib().kvp_paged_decode(ctypes.byref(pages), q, q_token, q_head, n_q_heads, table, table_width, lengths, n_seqs,
+                                  softmax_scale, out, workspace, workspace_bytes, stream)
 
 
 def kvp_free_cache(handle):

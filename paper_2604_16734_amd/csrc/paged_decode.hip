@@ -1,0 +1,521 @@
+// One decode step of many sequences, each over its own pages (kvp_paged_decode): out = softmax(scale q K^T) V with one query row per
+// query head.
+//
+// Bound by HBM: every key and value is read once and meets the G query heads of its KV head, 4 G flops for two numbers.  So what counts is
+// that every CU has loads on their way all the time, and that none of them has more to do than the others.
+//
+// Who does what.  The lengths are on the device, and the host plans nothing: pages.h deals the units of all sequences, tiles of 128 keys of
+// one KV head, to a fixed number of workgroups, as many as the chip holds at once, in equal shares; a workgroup finds its share by adding up the
+// lengths.  A piece that is all of a sequence and head is finished at once; the partial results (maximum, sum, unscaled output) of the others go
+// to the workspace, and a second kernel joins them, in the order of the workgroups, so that the same input gives the same bits.
+//
+// Within a tile each of the four waves takes 32 keys by itself, through two strips of LDS of its own, one for K and one for V: the next
+// tile's K is on its way as soon as this one's has been read, and the same for V; no barrier until a piece is done.  The rows come by
+// buffer_load ... lds, 16 at a time (no page is shorter), through descriptors that end with the last row there is: rows behind a
+// sequence's end, and of pages that do not exist, come as zeros without being read.
+//
+// Products.  S^T = K Q^T with 16x16x32 matrix instructions: rows are 16 keys, columns the query heads of the KV head (up to 16; the columns
+// beyond repeat the last one and are dropped).  A lane has four neighbouring keys of one query head of each 16, and these eight exponentials are, as they lie, its
+// part of the second operand of O^T = V^T P^T, whose first comes out of LDS by transposing reads in the same order of keys.  e4m3 numbers
+// become bf16 on the way from LDS to the matrix instruction, exactly; the powers of two of the rows are applied to the logits (K) and to the
+// weights (V), exactly, too.  Sums and maxima are in fp32; weights are rounded to bf16 for the product only.
+#include <type_traits>
+
+#include "mfma_tools.h"
+#include "serve.h"
+
+namespace kvp {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = kPagedTile / kWaves;      // keys of a wave's part of a tile
+constexpr int kHeads = 16;                     // columns of the products
+static_assert(kKeys == 32, "two blocks of 16 keys");
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+template <int D, bool kE4m3>
+struct Shape {
+  static constexpr int kRow = kE4m3 ? D : 2 * D;                  // bytes of a row in the pages
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kLoads = kRow / 64;                        // of 1 KiB, for 16 rows
+  static constexpr int kStrip = kKeys * kRow;
+  static constexpr int kExps = kE4m3 ? 256 : 0;
+  static constexpr int kWaveBytes = 2 * kStrip + kExps;
+  static constexpr int kLds = kWaves * kWaveBytes;
+  static constexpr int kPerCu = kLds > 40 * 1024 ? 2 : 4;         // workgroups of a CU
+  // what a wave leaves of a piece lies over its strips: the output as it is in the accumulators, then maxima and sums
+  static constexpr int kOut = kHeads * D * 4;
+  static constexpr int kStat = kE4m3 ? 2 * kStrip : kOut;
+  static_assert(kOut <= 2 * kStrip && kStat + 2 * kHeads * 4 <= kWaveBytes, "room for a piece");
+  static_assert(kLds <= 64 * 1024, "LDS that a kernel has without asking");
+};
+
+// In LDS the 16-byte chunk ch of row r lies at position ch ^ f(r), for reads free of bank conflicts.  K is read in chunks of one
+// column, 16 rows at a time; V by transposing reads of 8 bytes, of which half a wave's touch eight rows (bf16: 0 .. 7) or 16 (e4m3: 0 .. 7
+// and 16 .. 23).
+template <int kRow>
+__device__ __forceinline__ int k_swizzle(int row) { return row / (256 / kRow) % (kRow / 16); }
+template <int kRow, bool kE4m3>
+__device__ __forceinline__ int v_swizzle_of(int row) {
+  if constexpr (!kE4m3) return 2 * (row / (256 / kRow) % (kRow / 32));
+  else return row / (256 / kRow) % (kRow / 32) + kRow / 32 * (row / 16 % 2);
+}
+
+// eight e4m3 numbers as bf16, exactly
+__device__ __forceinline__ bf16x8 eight_of_e4m3(unsigned lo, unsigned hi) {
+  const u32x4 w = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true))};
+  return __builtin_bit_cast(bf16x8, w);
+}
+// 2^e of the i-th of four exponents
+__device__ __forceinline__ float power_of(unsigned exps, int i) {
+  return __uint_as_float((i < 3 ? exps << (23 - 8 * i) : exps >> 1) & 0x7F800000u);
+}
+// two transposing reads: four keys of this lane's channel, and the four that lie `rows` bytes further
+__device__ __forceinline__ bf16x8 lds_read_vt16(const unsigned char* p, int rows) {
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 __attribute__((address_space(3)))*)(p));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 __attribute__((address_space(3)))*)(p + rows));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// ---- where the units of the sequences begin, in all lanes of a wave
+__device__ __forceinline__ int length_of(const PagedDecodeArgs& a, int seq) {
+  return seq < a.n_seqs ? min(max(a.lengths[seq], 0), a.width << a.pool.shift) : 0;
+}
+__device__ __forceinline__ unsigned sum_of_wave(unsigned x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x += (unsigned)__shfl_xor((int)x, d);
+  return x;
+}
+__device__ __forceinline__ unsigned sum_before(unsigned x, int lane) {       // of the lanes up to and with this one
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const unsigned y = (unsigned)__shfl_up((int)x, d);
+    x += lane >= d ? y : 0u;
+  }
+  return x;
+}
+
+template <int D, bool kE4m3>
+__global__ void __launch_bounds__(kThreads, (Shape<D, kE4m3>::kPerCu * kWaves / 4))
+paged_decode_kernel(const PagedDecodeArgs a) {
+  using S = Shape<D, kE4m3>;
+  constexpr int kRow = S::kRow, kChunks = S::kChunks, kLoads = S::kLoads;
+  constexpr int kSteps = D / 32;                 // products with K of a block of 16 keys
+  constexpr int kTiles = D / 16;                 // channel tiles of the output
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // ---- this workgroup's share, and the sequence that it begins in
+  unsigned mine = 0;
+  for (int s = lane; s < a.n_seqs; s += 64) mine += (unsigned)paged_tiles(length_of(a, s));
+  const unsigned units = (unsigned)__builtin_amdgcn_readfirstlane(sum_of_wave(mine)) * (unsigned)a.pool.n_heads;
+  const unsigned share = (unsigned)__builtin_amdgcn_readfirstlane(paged_share(units, (unsigned)a.workgroups));
+  unsigned at = blockIdx.x * share;
+  if (at >= units) return;
+  const unsigned end = min(units, at + share);
+  // of 64 sequences at a time: lengths, and the units before each
+  int group0 = 0, length = length_of(a, lane);
+  unsigned before = 0, tiles = (unsigned)paged_tiles(length) * (unsigned)a.pool.n_heads, upto = sum_before(tiles, lane);
+  auto next_group = [&]() __attribute__((always_inline)) {
+    before += (unsigned)__builtin_amdgcn_readlane(upto, 63);
+    group0 += 64;
+    length = length_of(a, group0 + lane);
+    tiles = (unsigned)paged_tiles(length) * (unsigned)a.pool.n_heads;
+    upto = sum_before(tiles, lane);
+  };
+
+  // ---- LDS: [wave][K strip, V strip, exponents]
+  unsigned char* const k_strip = lds + wave * S::kWaveBytes;
+  unsigned char* const v_strip = k_strip + S::kStrip;
+  unsigned char* const exps = v_strip + S::kStrip;
+  const unsigned lds_at =
+      __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) void*)lds) + (unsigned)(wave * S::kWaveBytes);
+
+  // ---- global -> LDS.  Load i of 16 rows brings in rows 1024 / kRow * i + ..; its immediate offset moves both of its addresses by 1 KiB.
+  // (Inline assembly, and waits of this kernel's own: the compiler would have every read of LDS wait for all loads.  s_nop: a load may read a
+  // scalar register five wait states after a vector instruction has written it.)
+  unsigned k_lane[kLoads], v_lane[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int sub = lane / kChunks, pos = lane % kChunks, row = 1024 / kRow * i + sub;
+    k_lane[i] = (unsigned)(sub * kRow + 16 * (pos ^ k_swizzle<kRow>(row)));
+    v_lane[i] = (unsigned)(sub * kRow + 16 * (pos ^ v_swizzle_of<kRow, kE4m3>(row)));
+  }
+  auto load_rows = [&](u32x4 buffer, const unsigned (&of)[kLoads], unsigned flip, unsigned to) __attribute__((always_inline)) {
+    if constexpr (kLoads == 4)
+      asm volatile("s_mov_b32 m0, %5\n\ts_nop 3\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
+                   "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds" ::"v"(of[0] ^ flip), "v"(of[1] ^ flip), "v"(of[2] ^ flip),
+                   "v"(of[3] ^ flip), "s"(buffer), "s"(to)
+                   : "m0", "memory");
+    else if constexpr (kLoads == 2)
+      asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\t"
+                   "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds" ::"v"(of[0] ^ flip), "v"(of[1] ^ flip), "s"(buffer), "s"(to)
+                   : "m0", "memory");
+    else
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\t"
+                   "buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of[0] ^ flip), "s"(buffer), "s"(to)
+                   : "m0", "memory");
+  };
+  auto buffer_at = [&](const char* base, int rows) __attribute__((always_inline)) -> u32x4 {
+    const unsigned long long x = (unsigned long long)base;
+    // (through the first lane: for the compiler a quotient is no scalar, and neither is what follows from it)
+    return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)x), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32) & 0xFFFFu),
+                 (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(rows * kRow)), 0x00020000u};
+  };
+  auto wait_all_but = [&](auto newest) __attribute__((always_inline)) {
+    constexpr int k = decltype(newest)::value;
+    static_assert(k < 16);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | k);
+    asm volatile("" ::: "memory");
+  };
+  auto strips_read = [&]() __attribute__((always_inline)) {          // what was read from LDS is in registers
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  typedef std::integral_constant<int, 2 * kLoads + (kE4m3 ? 1 : 0)> KLoads;      // of a tile: exponents and K
+  typedef std::integral_constant<int, 2 * kLoads> VLoads;
+  typedef std::integral_constant<int, 0> None;
+
+  // ---- where the fragments are
+  int k_off[kSteps], v_off[kTiles];
+  if constexpr (!kE4m3) {
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) k_off[st] = l16 * kRow + 16 * ((4 * st + g) ^ k_swizzle<kRow>(l16));
+    const int row = 4 * g + l16 / 4;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+      v_off[dt] = row * kRow + 16 * ((2 * dt + l16 % 4 / 2) ^ v_swizzle_of<kRow, kE4m3>(row)) + 8 * (l16 & 1);
+  } else {
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) k_off[st] = l16 * kRow + 16 * ((4 * (st / 2) + g) ^ k_swizzle<kRow>(l16));      // 16 channels: two steps
+    const int key = l16 / 2, row = key < 4 ? 4 * g + key : 16 + 4 * g + key - 4;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) v_off[dt] = row * kRow + 16 * (dt ^ v_swizzle_of<kRow, kE4m3>(row)) + 8 * (l16 & 1);
+  }
+  const float sl2 = a.scale_log2;
+
+  // ---- pieces
+  int seq = -1, n_keys = 0;
+  unsigned seq_first = 0, seq_end = 0;
+  while (at < end) {
+    if (seq < 0 || at >= seq_end) {               // the sequence of unit `at`
+      while (before + (unsigned)__builtin_amdgcn_readlane(upto, 63) <= at && group0 + 64 < a.n_seqs) next_group();
+      const int i = __builtin_ctzll(__ballot(before + upto > at));
+      seq = group0 + i;
+      n_keys = __builtin_amdgcn_readlane(length, i);
+      seq_end = before + (unsigned)__builtin_amdgcn_readlane(upto, i);
+      seq_first = seq_end - (unsigned)__builtin_amdgcn_readlane(tiles, i);
+    }
+    const unsigned n_tiles = (unsigned)paged_tiles(n_keys);
+    const int head = __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
+    const unsigned first = seq_first + (unsigned)head * n_tiles;      // the first unit of this sequence and head
+    const int t0 = (int)(at - first), t1 = (int)(min(end, first + n_tiles) - first);
+    const int32_t* const row_of_table = a.table + (size_t)seq * a.width;
+
+    // the page numbers of 64 columns from col0 on; -1: no such page
+    int col0 = 0, ids = -1;
+    auto load_ids = [&](int col) __attribute__((always_inline)) {
+      col0 = col;
+      const int id = col + lane < a.width ? row_of_table[col + lane] : -1;
+      ids = id < a.pool.n_pages ? id : -1;
+      asm volatile("" : "+v"(ids));               // here, not where it is used: the wait there would be for all loads, every time
+    };
+    const int kb0 = kPagedTile * t0 + kKeys * wave;
+    if (kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
+
+    // Q: second operand, column l16 of the products; channels in the order of K's fragments
+    bf16x8 qf[kSteps];
+    {
+      const u16* const q = a.q + seq * a.q_token + (head * a.group + min(l16, a.group - 1)) * a.q_head;
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        const int ch = kE4m3 ? 16 * (4 * (st / 2) + g) + 8 * (st % 2) : 32 * st + 8 * g;
+        qf[st] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + ch));
+      }
+    }
+    f32x4 o[kTiles];
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    // rows of the two blocks of a tile that take part, and where they are
+    struct Tile {
+      int rows[2];
+      unsigned long long at[2];                   // row numbers in the pages
+    };
+    auto tile_at = [&](int t) __attribute__((always_inline)) -> Tile {
+      const int kb = kPagedTile * t + kKeys * wave;
+      Tile x;
+      if (((kb + 16) >> a.pool.shift) - col0 >= 64) load_ids(kb >> a.pool.shift);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const PagePlace p = place_of(kb + 16 * b, a.pool.shift);
+        const int id = __builtin_amdgcn_readlane(ids, p.column - col0);
+        x.rows[b] = id < 0 ? 0 : min(16, max(0, n_keys - kb - 16 * b));
+        x.at[b] = page_row(max(id, 0), a.pool.n_heads, head, p.offset, a.pool.shift);
+      }
+      return x;
+    };
+    auto issue_k = [&](const Tile& x) __attribute__((always_inline)) {
+      if constexpr (kE4m3) {                      // four exponents a lane: of block lane / 4 % 2, K's and V's
+        const unsigned long long row = lane & 4 ? x.at[1] : x.at[0];
+        const uint8_t* const src = (lane & 8 ? a.pool.v_exp : a.pool.k_exp) + row + 4 * (lane & 3);
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_at + 2 * S::kStrip) : "m0", "memory");
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.k + x.at[b] * kRow, x.rows[b]), k_lane, 0, lds_at + b * 16 * kRow);
+    };
+    auto issue_v = [&](const Tile& x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        load_rows(buffer_at(a.pool.v + x.at[b] * kRow, x.rows[b]), v_lane, b ? 16u * (unsigned)v_swizzle_of<kRow, kE4m3>(16) : 0u,
+                  lds_at + S::kStrip + b * 16 * kRow);
+    };
+
+    const int my_end = min(t1, (n_keys - kKeys * wave + kPagedTile - 1) / kPagedTile);      // tiles in which this wave has keys
+    Tile next{};
+    if (t0 < my_end) {
+      next = tile_at(t0);
+      issue_k(next);
+      issue_v(next);
+    }
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) asm volatile("" : "+v"(qf[st]));         // likewise
+    for (int t = t0; t < my_end; ++t) {
+      const Tile now = next;
+      const bool more = t + 1 < my_end;
+      // ---- logits
+      wait_all_but(VLoads{});
+      unsigned k_exp[2], v_exp[2];
+      if constexpr (kE4m3) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          k_exp[b] = *reinterpret_cast<const unsigned*>(exps + 4 * (4 * b + g));
+          v_exp[b] = *reinterpret_cast<const unsigned*>(exps + 4 * (8 + 4 * b + g));
+        }
+      }
+      f32x4 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!kE4m3) {
+#pragma unroll
+          for (int st = 0; st < kSteps; ++st) {
+            const bf16x8 kf = *reinterpret_cast<const bf16x8*>(k_strip + b * 16 * kRow + k_off[st]);
+            s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], s[b], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int st = 0; st < kSteps; st += 2) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(k_strip + b * 16 * kRow + k_off[st]);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+              s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_of_e4m3(w[2 * half], w[2 * half + 1]), qf[st + half], s[b], 0, 0, 0);
+          }
+        }
+      }
+      // K has been read; and a vector instruction may read a product 11 wait states after it, which the compiler does not see to in
+      // another basic block
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1])::"memory");
+      if (more) {
+        next = tile_at(t + 1);
+        issue_k(next);
+      }
+      // ---- weights
+      const bool masked = now.rows[0] + now.rows[1] < kKeys;
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (kE4m3) s[b][r] *= power_of(k_exp[b], r);
+          if (masked) s[b][r] = 4 * g + r < now.rows[b] ? s[b][r] : -INFINITY;
+          top = fmaxf(top, s[b][r]);
+        }
+      {
+        float y = top;
+        swap_lanes<16>(top, y);
+        top = fmaxf(top, y);
+        y = top;
+        swap_lanes<32>(top, y);
+        top = fmaxf(top, y);
+      }
+      if (__any(top > m)) {                       // a larger logit: what has been added up is brought onto it
+        const float m_new = fmaxf(m, top);
+        const float by = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
+        m = m_new;
+        l *= by;
+#pragma unroll
+        for (int dt = 0; dt < kTiles; ++dt) o[dt] *= by;
+      }
+      const float minus = m == -INFINITY ? 0.f : -m * sl2;
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], sl2, minus));
+        l += p[i];
+        if constexpr (kE4m3) {
+          p[i] *= power_of(v_exp[i / 4], i % 4);
+          if (masked) p[i] = 4 * g + i % 4 < now.rows[i / 4] ? p[i] : 0.f;      // (no row, no exponent)
+        }
+      }
+      const u32x4 pw = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+      // ---- values
+      if (more) wait_all_but(KLoads{});
+      else wait_all_but(None{});
+#pragma unroll
+      for (int dt = 0; dt < kTiles; ++dt) {
+        bf16x8 vf;
+        if constexpr (!kE4m3) vf = lds_read_vt16(v_strip + v_off[dt], 16 * kRow);
+        else {
+          const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(v_strip + v_off[dt]));
+          vf = eight_of_e4m3((unsigned)w[0], (unsigned)w[1]);
+        }
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[dt], 0, 0, 0);
+      }
+      strips_read();
+      if (more) issue_v(next);
+    }
+
+    // ---- the four waves' results of the piece, joined
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[dt]));        // (as above)
+    {
+      float y = l;
+      swap_lanes<16>(l, y);
+      l += y;
+      y = l;
+      swap_lanes<32>(l, y);
+      l += y;
+    }
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) reinterpret_cast<f32x4*>(k_strip)[64 * dt + lane] = o[dt];
+    if (lane < kHeads) {
+      float* const stat = reinterpret_cast<float*>(k_strip + S::kStat);
+      stat[lane] = m;
+      stat[kHeads + lane] = l;
+    }
+    __syncthreads();
+    const bool whole = piece_is_whole(first, n_tiles, share);
+    const size_t slot = (size_t)piece_slot(first, blockIdx.x, share) * a.group;
+#pragma unroll
+    for (int i = 0; i < 64 * kTiles / kThreads; ++i) {
+      const int item = kThreads * i + threadIdx.x, column = item % 16, ch = 16 * (item / 64) + 4 * (item / 16 % 4);
+      if (column >= a.group) continue;
+      float top = -INFINITY, f[kWaves], total = 0.f;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, reinterpret_cast<const float*>(lds + w * S::kWaveBytes + S::kStat)[column]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float* const stat = reinterpret_cast<const float*>(lds + w * S::kWaveBytes + S::kStat);
+        f[w] = __builtin_amdgcn_exp2f((stat[column] - (top == -INFINITY ? 0.f : top)) * sl2);
+        total += f[w] * stat[kHeads + column];
+        sum += f[w] * reinterpret_cast<const f32x4*>(lds + w * S::kWaveBytes)[item];
+      }
+      if (whole) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const u32x2 y = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+        *reinterpret_cast<u32x2*>(a.out + ((size_t)seq * a.n_q_heads + head * a.group + column) * D + ch) = y;
+      } else {
+        *reinterpret_cast<f32x4*>(a.partial + (slot + column) * D + ch) = sum;
+        if (ch == 0) {
+          float* const stat = a.partial + (size_t)2 * a.workgroups * a.group * D + 2 * (slot + column);
+          stat[0] = top * sl2;
+          stat[1] = total;
+        }
+      }
+    }
+    __syncthreads();
+    at = first + (unsigned)t1;
+  }
+}
+
+// ---- the pieces of one sequence and query head, joined; a sequence without keys has zeros
+template <int D>
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedDecodeArgs a) {
+  constexpr int kLanes = D / 4, kSlots = kThreads / kLanes;       // lanes of a slot's row; slots at a time
+  __shared__ f32x4 rows[kSlots][kLanes];
+  __shared__ float tops[kSlots], sums[kSlots];
+  const int lane = threadIdx.x & 63, hq = blockIdx.x, seq = blockIdx.y, head = hq / a.group, column = hq - head * a.group;
+  unsigned mine = 0, mine_before = 0;
+  for (int s = lane; s < a.n_seqs; s += 64) {
+    const unsigned t = (unsigned)paged_tiles(length_of(a, s));
+    mine += t;
+    mine_before += s < seq ? t : 0u;
+  }
+  const unsigned units = sum_of_wave(mine) * (unsigned)a.pool.n_heads;
+  const unsigned n_tiles = (unsigned)paged_tiles(length_of(a, seq)), share = paged_share(units, (unsigned)a.workgroups);
+  const unsigned first = sum_of_wave(mine_before) * (unsigned)a.pool.n_heads + (unsigned)head * n_tiles;
+  if (n_tiles > 0 && piece_is_whole(first, n_tiles, share)) return;
+  const int sub = threadIdx.x / kLanes, piece = threadIdx.x % kLanes;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (n_tiles > 0) {
+    const unsigned w1 = (first + n_tiles - 1) / share;
+    for (unsigned w = first / share + (unsigned)sub; w <= w1; w += kSlots) {
+      const size_t slot = (size_t)piece_slot(first, w, share) * a.group + column;
+      const float* const stat = a.partial + (size_t)2 * a.workgroups * a.group * D + 2 * slot;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.partial + slot * D + 4 * piece);
+      const float top = fmaxf(m, stat[0]), use = top == -INFINITY ? 0.f : top;
+      const float f0 = __builtin_amdgcn_exp2f(m - use), f1 = __builtin_amdgcn_exp2f(stat[0] - use);
+      o = o * f0 + x * f1;
+      l = l * f0 + stat[1] * f1;
+      m = top;
+    }
+  }
+  rows[sub][piece] = o;
+  if (piece == 0) {
+    tops[sub] = m;
+    sums[sub] = l;
+  }
+  __syncthreads();
+  if (sub != 0) return;
+  float top = -INFINITY, total = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) top = fmaxf(top, tops[i]);
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    const float f = __builtin_amdgcn_exp2f(tops[i] - (top == -INFINITY ? 0.f : top));
+    total += f * sums[i];
+    sum += f * rows[i][piece];
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const u32x2 y = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+  *reinterpret_cast<u32x2*>(a.out + ((size_t)seq * a.n_q_heads + hq) * D + 4 * piece) = y;
+}
+
+template <int D, bool kE4m3>
+hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3>), dim3(a.workgroups), dim3(kThreads), (Shape<D, kE4m3>::kLds), s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(paged_join_kernel<D>, dim3(a.n_q_heads, a.n_seqs), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+constexpr int kCus = 256;
+
+}  // namespace
+
+// as many as the chip holds at once
+int paged_decode_workgroups(int head_dim, bool e4m3) {
+  if (head_dim == 128) return kCus * (e4m3 ? Shape<128, true>::kPerCu : Shape<128, false>::kPerCu);
+  return kCus * (e4m3 ? Shape<64, true>::kPerCu : Shape<64, false>::kPerCu);
+}
+
+hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s) {
+  if (head_dim == 128) return e4m3 ? launch<128, true>(a, s) : launch<128, false>(a, s);
+  return e4m3 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+}
+
+}  // namespace kvp

@@ -70,9 +70,48 @@ int page_rows(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_b
   return code_of(write ? launch_page_write(a, pages->head_dim, e4m3, s) : launch_page_read(a, pages->head_dim, e4m3, s));
 }
 
+bool valid_group(int32_t n_q_heads, int32_t n_kv_heads) { return n_q_heads >= 1 && n_kv_heads >= 1 && n_q_heads % n_kv_heads == 0; }
+bool valid_scale(float s) { return s >= 0.f && !std::isinf(s); }
+float scale_log2_of(float scale, int head_dim) { return (scale > 0.f ? scale : 1.f / std::sqrt((float)head_dim)) * 1.4426950408889634f; }
+
 }  // namespace
 
+// What a decode step needs: two places for partial results per workgroup, each of a KV head's query heads.
+static size_t paged_decode_bytes(const kvp_pages& p, int group) {
+  return (size_t)2 * paged_decode_workgroups(p.head_dim, p.format == KVP_PAGE_E4M3) * group * (p.head_dim + 2) * sizeof(float);
+}
+
 extern "C" {
+
+size_t kvp_paged_decode_bytes(const kvp_pages* pages, int32_t n_q_heads) {
+  if (!valid_pages(pages) || !valid_group(n_q_heads, pages->n_kv_heads) || n_q_heads / pages->n_kv_heads > kDecodeGroupLimit) return 0;
+  return paged_decode_bytes(*pages, n_q_heads / pages->n_kv_heads);
+}
+
+int kvp_paged_decode(const kvp_pages* pages, const void* q, int64_t q_token, int64_t q_head, int32_t n_q_heads,
+                     const int32_t* table, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
+                     float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!valid_pages(pages) || !valid_table(table, table_width, pages->page_size, n_seqs)) return KVP_EINVAL;
+  if (!valid_group(n_q_heads, pages->n_kv_heads) || n_q_heads / pages->n_kv_heads > kDecodeGroupLimit || n_q_heads > 65535) return KVP_EINVAL;
+  const unsigned long long tiles = ((unsigned long long)table_width * (unsigned)pages->page_size + kPagedTile - 1) / kPagedTile;
+  if (tiles * (unsigned)n_seqs > (1ull << 31) / (unsigned)pages->n_kv_heads) return KVP_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lengths, 4) || !aligned(workspace, 16)) return KVP_EINVAL;
+  if (!valid_strides(q_token, q_head) || !valid_scale(softmax_scale)) return KVP_EINVAL;
+  if (workspace_bytes < kvp_paged_decode_bytes(pages, n_q_heads)) return KVP_ENOMEM;
+  PagedDecodeArgs a{};
+  const bool e4m3 = pages->format == KVP_PAGE_E4M3;
+  a.pool = pool_of(*pages);
+  a.q = static_cast<const u16*>(q);
+  a.out = static_cast<u16*>(out);
+  a.table = table; a.lengths = lengths;
+  a.partial = static_cast<float*>(workspace);
+  a.q_token = q_token; a.q_head = q_head;
+  a.width = table_width; a.n_seqs = n_seqs; a.n_q_heads = n_q_heads;
+  a.group = n_q_heads / pages->n_kv_heads;
+  a.workgroups = paged_decode_workgroups(pages->head_dim, e4m3);
+  a.scale_log2 = scale_log2_of(softmax_scale, pages->head_dim);
+  return code_of(launch_paged_decode(a, pages->head_dim, e4m3, static_cast<hipStream_t>(stream)));
+}
 
 int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
                    int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream) {

@@ -26,6 +26,21 @@ struct PageRowsArgs {
   Divisor by_heads;
 };
 
+struct PagedDecodeArgs {
+  Pool pool;
+  const u16* q;
+  u16* out;                   // [n_seqs][n_q_heads][D]
+  const int32_t* table;
+  const int32_t* lengths;
+  float* partial;             // [2 * workgroups][group][D], then [2 * workgroups][group][2]: maximum (log2 domain) and sum
+  long long q_token, q_head;
+  int width, n_seqs, n_q_heads, group;
+  int workgroups;
+  float scale_log2;
+};
+int paged_decode_workgroups(int head_dim, bool e4m3);
+hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);
+
 hipError_t launch_page_write(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
 hipError_t launch_page_read(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
 

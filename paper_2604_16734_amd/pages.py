@@ -113,3 +113,35 @@ class Pages:
     def read(self, k, v, seq_begin, table, first=None, stream=None):
         """The way back, into k and v (kvp_page_read)."""
         self._rows("read", k, v, seq_begin, table, first, stream)
+
+    def workspace(self, n_q_heads):
+        """Room for the partial results of a decode step with this many query heads; steps that may overlap need one each."""
+        import torch
+        nbytes = self._lib.kvp_paged_decode_bytes(self._ref, n_q_heads)
+        _need(nbytes > 0, "Pages.workspace: n_q_heads")
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def decode(self, q, table, lengths, out=None, softmax_scale=0.0, workspace=None, stream=None):
+        """One token of every sequence: q [n_seqs, n_q_heads, head_dim] over tokens 0 .. lengths[s] - 1 of the pages table[s]
+        (kvp_paged_decode).  Without a workspace one is allocated for the call."""
+        import torch
+        n_seqs, device = lengths.numel(), self.device
+        _need(q.dim() == 3 and table.dim() == 2, "Pages.decode: q and table")
+        n_q_heads, what = q.shape[1], "Pages.decode: "
+        shape = (n_seqs, n_q_heads, self.head_dim)
+        q_at, q_token, q_head = _numbers(q, shape, device, what + "q")
+        table_at = _whole(table, (n_seqs, table.shape[1]), device, what + "table")
+        lengths_at = _whole(lengths, (n_seqs,), device, what + "lengths")
+        with _On(device, stream) as handle:
+            if out is None:
+                out = torch.empty(shape, dtype=torch.bfloat16, device=device)
+            else:
+                _need(out.dtype is torch.bfloat16 and out.device == device and out.shape == shape and out.is_contiguous(), what + "out")
+            if workspace is None:
+                workspace = self.workspace(n_q_heads)
+            _need(workspace.device == device and workspace.is_contiguous(), what + "workspace")
+            rc = self._lib.kvp_paged_decode(self._ref, q_at, q_token, q_head, n_q_heads, table_at, table.shape[1], lengths_at, n_seqs,
+                                            softmax_scale, out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle)
+        if rc:
+            raise KvpError(rc, "kvp_paged_decode")
+        return out

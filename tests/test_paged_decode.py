@@ -1,0 +1,250 @@
+"""One decode step of many sequences over their pages, against softmax attention in 64 bits; refusals."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_16734_amd as K
+from tests.test_pages import BAD_PAGES, DEV, P16, P4, Pool, _pages, gpu, int32
+
+
+def reference(q, pool, table, lengths, n_pages, page, scale):
+    """(out, size): softmax attention in 64 bits, and the same with the values' magnitudes: what errors of the weights are relative to.
+    Also the largest sum of magnitudes of a logit's products, times the scale."""
+    n_seqs, hq, d = q.shape
+    hkv = pool.k.shape[1]
+    out, size, most = np.zeros(q.shape), np.zeros(q.shape), 0.0
+    for s in range(n_seqs):
+        keys = []
+        for p in range(max(0, min(lengths[s], table.shape[1] * page))):
+            number = int(table[s, p // page])
+            if 0 <= number < n_pages:
+                keys.append((number, p % page))
+        if not keys:
+            continue
+        pages, at = np.array(keys).T
+        for h in range(hkv):
+            k, v = (getattr(pool, n)[pages, h, at] for n in "kv")
+            if pool.e4m3:
+                k, v = (x * np.exp2(getattr(pool, n + "_exp")[pages, h, at] - 127.0)[:, None] for x, n in ((k, "k"), (v, "v")))
+            of = slice(h * (hq // hkv), (h + 1) * (hq // hkv))
+            logits = q[s, of] @ k.T * scale
+            most = max(most, float((np.abs(q[s, of]) @ np.abs(k).T).max()) * scale)
+            w = np.exp(logits - logits.max(axis=1, keepdims=True))
+            w /= w.sum(axis=1, keepdims=True)
+            out[s, of], size[s, of] = w @ v, w @ np.abs(v)
+    return out, size, most
+
+
+def check(out, ref, size, most, d):
+    """Half a bf16 step for every weight and for the result; a logit is off by d fp32 roundings of its products at most and the weight
+    by as much relatively, once in the sum and once in the product; and a dozen fp32 roundings of the rest."""
+    half, fp32 = 2.0 ** -8, 2.0 ** -24
+    tol = size * (half + 2 * d * most * fp32 + 64 * fp32) + np.abs(ref) * half + 1e-30
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    worst = np.max(np.abs(got - ref) / tol)
+    assert worst <= 1.0, worst
+
+
+def a_batch(gen, lengths, hkv, d, page, e4m3, spare=3):
+    """Pages of these sequences in random order with numbers in their rows, and NaNs in all others."""
+    counts = [max(1, -(-n // page)) for n in lengths]
+    width, n_pages = max(counts), sum(counts) + spare
+    order = torch.randperm(n_pages, generator=gen)
+    table = torch.full((len(lengths), width), -1, dtype=torch.int32)
+    pages = K.Pages.empty(n_pages, hkv, d, page, e4m3, DEV)
+    for t in (pages.k, pages.v):
+        t.view(torch.uint8).fill_(0xFF)                     # NaN in either format
+    if e4m3:
+        pages.k_exp.fill_(255), pages.v_exp.fill_(255)
+    i = 0
+    for s, c in enumerate(counts):
+        table[s, :c] = order[i:i + c].int()
+        i += c
+    table = table.to(DEV)
+    begin = int32(np.concatenate([[0], np.cumsum(lengths)]).tolist())
+    n = sum(lengths)
+    k, v = (torch.randn(n, hkv, d, generator=gen).to(torch.bfloat16).to(DEV) for _ in range(2))
+    if n:
+        pages.write(k, v, begin, table)
+    return pages, table
+
+
+SHAPES = [(4, 4, 64), (32, 8, 128), (7, 1, 128), (16, 1, 64), (10, 2, 128), (16, 1, 128), (6, 2, 64), (28, 4, 128)]
+LENGTHS = [[1], [16, 17, 0, 31], [127, 128, 129, 130, 64], [1000], [5000, 3, 700], [0, 0]]
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("lengths", LENGTHS)
+@pytest.mark.parametrize("hq,hkv,d", SHAPES)
+def test_against_64_bits(hq, hkv, d, lengths, page, e4m3):
+    gen = torch.Generator().manual_seed(hq * 1000 + sum(lengths) + page)
+    pages, table = a_batch(gen, lengths, hkv, d, page, e4m3)
+    q = (1.5 * torch.randn(len(lengths), hq, d, generator=gen)).to(torch.bfloat16)
+    print("paged decode", hq, hkv, d, lengths, page, e4m3, flush=True)
+    work = pages.workspace(hq).fill_(0xFF)
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device=DEV)
+    pages.decode(q.to(DEV), table, int32(lengths), out=out, workspace=work)
+    torch.cuda.synchronize()
+    ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, page, d ** -0.5)
+    check(out, ref, size, most, d)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_pages_that_are_not_there_and_lengths_out_of_range(e4m3):
+    gen = torch.Generator().manual_seed(3)
+    page, hq, hkv, d, lengths = 32, 8, 2, 128, [200, 96, 33, 64, 500]          # (the second one's pages are full: it is taken further)
+    pages, table = a_batch(gen, lengths, hkv, d, page, e4m3)
+    q = torch.randn(len(lengths), hq, d, generator=gen).to(torch.bfloat16)
+    table[0, 0], table[0, 4], table[1, 1], table[2, 1], table[4, 3:11] = -1, pages.n_pages, -7, 2 ** 31 - 1, -2 ** 31
+    table[3] = -1                                          # none left
+    said = [200, 2 ** 31 - 1, 33, 64, 500]
+    table[1, 3:] = table[0, 2]                             # (what the longer length reaches)
+    for given in (said, [-5, 96, 0, -2 ** 31, 499]):
+        out = pages.decode(q.to(DEV), table, int32(given))
+        torch.cuda.synchronize()
+        ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), given, pages.n_pages, page, d ** -0.5)
+        check(out, ref, size, most, d)
+        assert not out[3].any()
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_sequences(e4m3):
+    gen = torch.Generator().manual_seed(8)
+    lengths = [int(x) for x in torch.randint(0, 400, (150,), generator=gen)]
+    lengths[:70] = [0] * 70
+    lengths[149] = 2500
+    pages, table = a_batch(gen, lengths, 2, 64, 16, e4m3)
+    q = torch.randn(150, 3, 6, 64, generator=gen).to(torch.bfloat16)
+    out = pages.decode(q.to(DEV)[:, 1], table, int32(lengths), softmax_scale=0.3)      # rows of another tensor
+    torch.cuda.synchronize()
+    ref, size, most = reference(q[:, 1].double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, 16, 0.3)
+    check(out, ref, size, most, 64)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_long_sequence_and_the_same_bits_again(e4m3):
+    """All workgroups on the pieces of one sequence; large logits, the largest of them last."""
+    gen = torch.Generator().manual_seed(9)
+    n, page, hq, hkv, d = 20011, 16, 8, 1, 128
+    pages, table = a_batch(gen, [n], hkv, d, page, e4m3)
+    q = (8 * torch.randn(1, hq, d, generator=gen)).to(torch.bfloat16).to(DEV)
+    row = 30 * q[:, :1] / q[:, :1].float().norm()
+    pages.write(row.to(torch.bfloat16), row.to(torch.bfloat16), int32([0, 1]), table, first=int32([n - 1]))
+    out = pages.decode(q, table, int32([n]))
+    again = [pages.decode(q, table, int32([n])) for _ in range(3)]
+    torch.cuda.synchronize()
+    ref, size, most = reference(q.double().cpu().numpy(), Pool(pages), table.cpu().numpy(), [n], pages.n_pages, page, d ** -0.5)
+    check(out, ref, size, most, d)
+    assert all(torch.equal(out.view(torch.int16), a.view(torch.int16)) for a in again)
+
+
+@gpu
+def test_numbers_that_are_not_finite_stay_with_their_sequence_and_head():
+    gen = torch.Generator().manual_seed(10)
+    pages, table = a_batch(gen, [300, 300], 2, 128, 64, False)
+    q = torch.randn(2, 4, 128, generator=gen).to(torch.bfloat16).to(DEV)
+    good = pages.decode(q, table, int32([300, 300]))
+    pages.v[table[0, 1], 1, 5, 7] = float("inf")
+    pages.k[table[1, 2], 0, 9] = float("nan")
+    out = pages.decode(q, table, int32([300, 300]))
+    torch.cuda.synchronize()
+    assert torch.equal(out[0, :2], good[0, :2]) and torch.equal(out[1, 2:], good[1, 2:])
+    assert torch.isinf(out[0, 2:, 7]).all() and torch.isfinite(out[0, 2:, :7]).all()
+    assert torch.isnan(out[1, :2]).all()
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_graph_of_steps_goes_on_with_other_lengths(e4m3):
+    """Write the token, attend, in a graph with a workspace that a second graph shares; eager work between the replays."""
+    gen = torch.Generator().manual_seed(11)
+    lengths, page, hq, hkv, d = [100, 0, 57], 16, 8, 2, 128
+    pages, table = a_batch(gen, [n + 40 for n in lengths], hkv, d, page, e4m3)
+    k, v = (torch.randn(3, hkv, d, generator=gen).to(torch.bfloat16).to(DEV) for _ in range(2))
+    q = torch.randn(3, hq, d, generator=gen).to(torch.bfloat16).to(DEV)
+    at, upto, begin, work = int32(lengths), int32([n + 1 for n in lengths]), int32([0, 1, 2, 3]), pages.workspace(hq)
+    outs = [torch.empty_like(q) for _ in range(2)]
+
+    def step(out):
+        pages.write(k, v, begin, table, first=at)
+        pages.decode(q, table, upto, out=out, workspace=work)
+        at.add_(1), upto.add_(1)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step(outs[0])                                      # token 0, eager, on another stream
+    torch.cuda.synchronize()
+    graphs = []
+    for out in outs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step(out)
+    for token in range(1, 13):
+        for t in (k, v, q):
+            t.copy_(torch.randn(t.shape, generator=gen))
+        graphs[token % 2].replay()
+        eager = pages.decode(q, table, int32([n + token + 1 for n in lengths]))
+        torch.cuda.synchronize()
+        ref, size, most = reference(q.double().cpu().numpy(), Pool(pages), table.cpu().numpy(), [n + token + 1 for n in lengths], pages.n_pages, page,
+                                    d ** -0.5)
+        check(outs[token % 2], ref, size, most, d)
+        assert torch.equal(eager, outs[token % 2])
+
+
+@gpu
+def test_nothing_behind_the_result_and_the_workspace_is_written():
+    gen = torch.Generator().manual_seed(12)
+    pages, table = a_batch(gen, [900, 40], 1, 64, 64, False)
+    q = torch.randn(2, 5, 64, generator=gen).to(torch.bfloat16).to(DEV)
+    nbytes = K.kvp_paged_decode_bytes(pages.of, 5)
+    room = torch.full((nbytes + 512,), 0xAB, dtype=torch.uint8, device=DEV)
+    out = torch.full((4, 5, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    pages.decode(q, table, int32([900, 40]), out=out[1:3], workspace=room[256:256 + nbytes])
+    torch.cuda.synchronize()
+    assert (out[0] == 3).all() and (out[3] == 3).all() and (out[1:3] != 3).any()
+    assert (room[:256] == 0xAB).all() and (room[256 + nbytes:] == 0xAB).all()
+
+
+def _decode(pages=None, **over):
+    of = dict(q=P16, q_token=512, q_head=128, n_q_heads=4, table=P4, table_width=4, lengths=P4, n_seqs=2, softmax_scale=0.0, out=P16, workspace=P16,
+              workspace_bytes=1 << 30)
+    of.update(over)
+    return K.kvp_paged_decode(pages or _pages(), *of.values())
+
+
+def test_refusals():
+    for bad in BAD_PAGES:
+        assert _decode(_pages(**bad)) == K.KVP_EINVAL, bad
+        assert K.kvp_paged_decode_bytes(_pages(**bad), 4) == 0
+    for bad in [dict(q=None), dict(q=P16 + 8), dict(q_token=12), dict(q_head=-8), dict(n_q_heads=3), dict(n_q_heads=0), dict(n_q_heads=34), dict(table=None),
+                dict(table_width=0), dict(table_width=1 << 25), dict(lengths=None), dict(lengths=P4 + 1), dict(n_seqs=0), dict(n_seqs=4097),
+                dict(softmax_scale=-1.0), dict(softmax_scale=math.inf), dict(softmax_scale=math.nan), dict(out=None), dict(out=P16 + 2), dict(workspace=None),
+                dict(workspace=P16 + 4), dict(table_width=1 << 24, n_seqs=4096)]:
+        assert _decode(**bad) == K.KVP_EINVAL, bad
+    need = K.kvp_paged_decode_bytes(_pages(), 4)
+    assert need > 0 and _decode(workspace_bytes=need - 1) == K.KVP_ENOMEM
+    assert K.kvp_paged_decode_bytes(_pages(), 3) == 0 and K.kvp_paged_decode_bytes(_pages(), 34) == 0
+    assert K.kvp_paged_decode_bytes(_pages(format=K.KVP_PAGE_E4M3), 32) > 0
+
+
+@gpu
+def test_refusals_of_tensors():
+    pages = K.Pages.empty(4, 2, 128, 64, False, DEV)
+    row = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16, device=DEV)
+    good = dict(q=row(2, 4, 128), table=int32([[0], [1]]), lengths=int32([0, 0]))
+    pages.decode(**good)
+    for bad in [dict(q=row(2, 4, 64)), dict(q=row(3, 4, 128)), dict(q=row(2, 3, 128)), dict(q=row(2, 4, 128).float()), dict(q=row(4, 128)),
+                dict(table=int32([[0]])), dict(lengths=int32([0, 0]).long()), dict(lengths=torch.zeros(2, dtype=torch.int32)), dict(out=row(2, 4, 64)),
+                dict(out=row(2, 4, 256)[..., :128]), dict(workspace=torch.empty(64, dtype=torch.uint8, device=DEV))]:
+        with pytest.raises(K.KvpError):
+            pages.decode(**dict(good, **bad))
+    torch.cuda.synchronize()
