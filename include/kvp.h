@@ -439,6 +439,36 @@ int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* 
 int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
                   int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream);
 
+/* Attention of whole prompts (Eq. 1), many of them packed one behind the other: rows
+ * seq_begin[s] .. seq_begin[s + 1] - 1 of q, k and v are those of prompt s, and row i
+ * attends to the rows of its own prompt up to i.
+ *   q, out    bf16, number c of head h of token t at t * token + h * head + c, with
+ *   k, v      strides of their own; out overlaps none of the others
+ *   seq_begin device [n_seqs + 1], not descending, from 0 to n_tokens at most (brought
+ *             into that range); rows of out that belong to no prompt are left as they were
+ * Query head h reads KV head h / (n_q_heads / n_kv_heads).  fp32 accumulation, rounded
+ * once; softmax_scale 0 means 1/sqrt(head_dim).  What a row does not see has no part in
+ * it, were it infinite.  n_tokens = 0 does nothing.  KVP_EINVAL also where
+ * (n_tokens / 128 + n_seqs) * n_q_heads passes 2^30, or rows from token to token are
+ * less than head_dim apart. */
+typedef struct kvp_prompts {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  const int32_t* seq_begin;
+  int64_t q_token, q_head;
+  int64_t k_token, k_head;
+  int64_t v_token, v_head;
+  int64_t out_token, out_head;
+  int32_t n_tokens, n_seqs;
+  int32_t n_q_heads;    /* multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  float softmax_scale;
+} kvp_prompts;
+int kvp_prompt_attention(const kvp_prompts* prompts, void* stream);
+
 /* One decode step of one layer for many sequences, each over its own pages (Eq. 1
  * with one query row per head, as kvp_decode_step):
  *   q          bf16, number c of head h of sequence s at s * q_token + h * q_head + c

@@ -15,7 +15,7 @@ from .binding import (  # noqa: F401
     kvp_profile_enable,
     kvp_profile_read, kvp_kernel_name, kvp_debug_totals, TOTALS, kvp_probe_mfma, kvp_probe_copy, kvp_free_cache,
     Cache, KVP_PAGE_BF16, KVP_PAGE_E4M3, KVP_MAX_SEQUENCES, KVP_MAX_PAGE_SIZE, KvpPages, KvpRows, kvp_page_write, kvp_page_read,
-    kvp_paged_decode_bytes, kvp_paged_decode,
+    kvp_paged_decode_bytes, kvp_paged_decode, KvpPrompts, kvp_prompt_attention,
 )
-from .pages import Pages  # noqa: F401
+from .pages import Pages, prompt_attention  # noqa: F401
 from .runtime import Prefill, LayerwisePrefill  # noqa: F401

@@ -56,6 +56,12 @@ class KvpRows(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("k_token", "k_head", "v_token", "v_head")] + [("n_tokens", ctypes.c_int32)]
 
 
+class KvpPrompts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "seq_begin")] + \
+               [(t + n, ctypes.c_int64) for t in ("q", "k", "v", "out") for n in ("_token", "_head")] + \
+               [(n, ctypes.c_int32) for n in ("n_tokens", "n_seqs", "n_q_heads", "n_kv_heads", "head_dim")] + [("softmax_scale", ctypes.c_float)]
+
+
 class KvpKernelStat(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("layers", ctypes.c_int64), ("total_ms", ctypes.c_double)]
 
@@ -142,6 +148,8 @@ def lib():
         L.kvp_paged_decode_bytes.argtypes = [P(KvpPages), i32]
         L.kvp_paged_decode.restype = ctypes.c_int
         L.kvp_paged_decode.argtypes = [P(KvpPages), vp, ctypes.c_int64, ctypes.c_int64, i32, vp, i32, vp, i32, ctypes.c_float, vp, vp, sz, vp]
+        L.kvp_prompt_attention.restype = ctypes.c_int
+        L.kvp_prompt_attention.argtypes = [P(KvpPrompts), vp]
         L.kvp_free_cache.restype = None
         L.kvp_free_cache.argtypes = [vp]
         _lib = L
@@ -344,6 +352,10 @@ def kvp_paged_decode(pages, q, q_token, q_head, n_q_heads, table, table_width, l
                      workspace_bytes, stream=0):
     return lib().kvp_paged_decode(ctypes.byref(pages), q, q_token, q_head, n_q_heads, table, table_width, lengths, n_seqs,
                                   softmax_scale, out, workspace, workspace_bytes, stream)
+
+
+def kvp_prompt_attention(prompts, stream=0):
+    return lib().kvp_prompt_attention(ctypes.byref(prompts), stream)
 
 
 def kvp_free_cache(handle):

@@ -1,0 +1,452 @@
+// Causal attention inside each of many prompts that lie one behind the other (kvp_prompt_attention), for gfx950: bf16 MFMA 32x32x16, K
+// and V tiles through LDS.
+//
+// Bound by the matrix cores for long prompts: 4 d flops for each pair of a row and a key that it sees, against 2 d numbers of K and V that serve
+// the 128 rows of a workgroup and come out of the L2 cache of its die.
+//
+// Formulation.  A wave owns 32 query rows of one head and works on the transposed problem, S^T = K Q^T and O^T = V^T P^T: in the 32x32
+// accumulator layout a lane then holds one query row, the softmax reference and sum are a number per lane, and the exponentiated
+// accumulators are, register for register, the second operand of the second product.  Accumulator register r of lane (g = lane / 32) holds key
+// 8 (r / 4) + 4 g + r % 4 of its 32; V is read out of LDS, transposed, in that order of keys.
+//
+// A workgroup is four waves, 128 neighbouring rows of one head, and two of them share a CU: what one waits for the other fills.  Tiles of 64 keys come by
+// buffer_load ... lds into two K and two V buffers, 64 KiB, row by row with the 16-byte chunks of a row swizzled by its number, so that all
+// reads are free of bank conflicts.  The descriptors end with the last row that a row of the workgroup sees: what lies behind it comes as zeros and costs
+// nothing.  Of tile t the wave takes the blocks of 32 keys X and Y; matrix and vector work overlap in program order:
+//   phase 1   MFMA: S_Y(t), O += P_Y(t-1) V     | vector: P_X(t) = exp(S_X(t) - m)
+//   barrier
+//   phase 2   MFMA: S_X(t+1), O += P_X(t) V     | vector: P_Y(t) = exp(S_Y(t) - m), the loads of K(t+2) and V(t+1)
+//
+// Softmax reference.  exp(S - m) is exact for any m as long as nothing overflows: a row takes the maximum of the first 32 keys that it
+// sees and O is never rescaled.  A row sum beyond 2^64 says that this did not do; a result that is not finite may also come from a value that the
+// row does not see, because 0 times infinity is no 0.  In both cases the wave takes its rows again the slow way, with a running maximum and
+// values only where they are seen.
+#include <type_traits>
+
+#include "mfma_tools.h"
+#include "serve.h"
+
+namespace kvp {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+static_assert(kPromptRows == 32 * kWaves, "rows of a workgroup");
+constexpr int kTileKeys = 64;
+
+template <int D>
+struct Shape {
+  static constexpr int kChunks = D / 8;                        // 16-byte chunks of a row
+  static constexpr int kRowsPerLoad = 64 / kChunks;
+  static constexpr int kLoads = kTileKeys / kWaves / kRowsPerLoad;      // of a wave, tensor and tile: 16 rows
+  static constexpr int kTile = kTileKeys * D;                  // numbers
+  static constexpr int kLds = 4 * kTile * 2;
+  static_assert(kLds <= 64 * 1024, "LDS that a kernel has without asking");
+};
+
+// Tile of 128 rows number `rank` of a list that goes through the sequences: each sequence's tiles, the last one, which sees most keys, first.
+struct PromptTile {
+  int begin, length, tile;            // the sequence's first row and its rows; length 0: no such tile
+};
+__device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, int lane) {
+  int before = 0;
+  for (int base = 0; base < a.n_seqs; base += 64) {
+    const int s = min(base + lane, a.n_seqs - 1);
+    const int begin = min(max(a.seq_begin[s], 0), a.n_tokens), end = min(max(a.seq_begin[s + 1], begin), a.n_tokens);
+    const int tiles = base + lane < a.n_seqs ? (end - begin + kPromptRows - 1) / kPromptRows : 0;
+    int upto = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(upto, d);
+      upto += lane >= d ? y : 0;
+    }
+    const unsigned long long there = __ballot(before + upto > rank);
+    if (there != 0) {
+      const int i = __builtin_ctzll(there);
+      return PromptTile{__builtin_amdgcn_readlane(begin, i), __builtin_amdgcn_readlane(end - begin, i),
+                        before + __builtin_amdgcn_readlane(upto, i) - 1 - rank};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return PromptTile{0, 0, 0};
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const PromptArgs a) {
+  using S = Shape<D>;
+  constexpr int kNK = D / 16, kNV = (D / 32) * 2, kND = D / 32;       // K and V fragments of a block of 32 keys; channel tiles
+  extern __shared__ __align__(16) unsigned char lds_raw[];
+  u16* const lds_k = reinterpret_cast<u16*>(lds_raw);              // [2][kTile]
+  u16* const lds_v = lds_k + 2 * S::kTile;                         // [2][kTile]
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // a die has heads of its own where they can be dealt out evenly: its L2 then holds the K and V of these alone
+  const int xcd = blockIdx.x % kXcds, item = blockIdx.x / kXcds;
+  int h, rank;
+  if (a.heads_per_xcd > 0) {
+    rank = (int)quotient((unsigned)item, a.by_heads);
+    h = xcd * a.heads_per_xcd + item - rank * a.heads_per_xcd;
+  } else {
+    rank = (int)quotient(blockIdx.x, a.by_heads);
+    h = (int)blockIdx.x - rank * a.n_q_heads;
+  }
+  const PromptTile pt = find_tile(a, rank, lane);
+  const int n = pt.length, wg_row = pt.tile * kPromptRows;
+  if (wg_row >= n) return;
+  const int hk = (int)quotient((unsigned)h, a.by_group);
+  const u16* const q_rows = a.q + pt.begin * a.q_token + h * a.q_head;
+  const u16* const k_rows = a.k + pt.begin * a.k_token + hk * a.k_head;
+  const u16* const v_rows = a.v + pt.begin * a.v_token + hk * a.v_head;
+  u16* const out_rows = a.out + pt.begin * a.out_token + h * a.out_head;
+  const int q0 = wg_row + 32 * wave;                    // this wave's first row; it may lie past the end
+  const int rows_end = min(n, wg_row + kPromptRows);
+  const int n_tiles = (rows_end + kTileKeys - 1) / kTileKeys;                              // of the workgroup
+  const int my_tiles = q0 < n ? (min(n, q0 + 32) + kTileKeys - 1) / kTileKeys : 0;        // that this wave sees
+  const int n_plain = min(my_tiles, (q0 + 1) / kTileKeys);                                // that all of its rows see whole
+  const float sl2 = a.scale_log2;
+
+  // ---- staging.  Wave w brings in rows 16 w .. 16 w + 15 of a tile; load j's immediate offset moves both of its addresses by 1 KiB, and the lane's part
+  // takes that back where rows lie further apart.  (Inline assembly, and waits of this kernel's own: the compiler would have every read of
+  // LDS wait for all loads.  s_nop: a load may read a scalar register five wait states after a vector instruction has written it.)
+  const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) void*)lds_raw);
+  auto lds_dst = [&](const u16* tile) __attribute__((always_inline)) -> unsigned {
+    return lds_at + 2u * (unsigned)((int)(tile - lds_k) + 16 * wave * D);
+  };
+  const int ld_sub = lane / S::kChunks, ld_pos = lane % S::kChunks;
+  unsigned k_lane[S::kLoads], v_lane[S::kLoads];
+#pragma unroll
+  for (int j = 0; j < S::kLoads; ++j) {
+    const int row = 16 * wave + S::kRowsPerLoad * j + ld_sub;
+    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks)) - 1024u * j;
+    v_lane[j] = (unsigned)row * a.v_bytes + 16u * (unsigned)(ld_pos ^ v_swizzle<D>(row)) - 1024u * j;
+  }
+  struct Feed {
+    unsigned long long at;
+    unsigned tile_bytes, row_bytes;
+    int rows;                          // from this tile's first one on
+  };
+  auto load_fed = [&](const Feed& f, const unsigned (&of)[S::kLoads], auto which, unsigned to) __attribute__((always_inline)) {
+    constexpr int j = decltype(which)::value;
+    const unsigned bytes = f.rows >= kTileKeys ? f.tile_bytes : f.rows > 0 ? (unsigned)(f.rows - 1) * f.row_bytes + 2u * D : 0u;
+    const u32x4 buffer = {(unsigned)f.at, (unsigned)(f.at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen offset:%3 lds" ::"v"(of[j]), "s"(buffer), "s"(to), "n"(1024 * j)
+                 : "m0", "memory");
+  };
+  auto move_on = [&](Feed& f) __attribute__((always_inline)) {
+    f.at += f.tile_bytes;
+    f.rows -= kTileKeys;
+  };
+  auto load_tile = [&](const Feed& f, const unsigned (&of)[S::kLoads], unsigned to) __attribute__((always_inline)) {
+    load_fed(f, of, std::integral_constant<int, 0>{}, to);
+    load_fed(f, of, std::integral_constant<int, 1>{}, to);
+    if constexpr (S::kLoads == 4) {
+      load_fed(f, of, std::integral_constant<int, 2>{}, to);
+      load_fed(f, of, std::integral_constant<int, 3>{}, to);
+    }
+  };
+  auto wait_all_but = [&](auto newest) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | decltype(newest)::value);
+    asm volatile("" ::: "memory");
+  };
+  typedef std::integral_constant<int, 0> None;
+
+  // ---- where the fragments are (in numbers)
+  int k_off[kNK], v_off[kND];
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ (l32 % S::kChunks)));
+  {
+    const int rsub = 4 * g + ((lane & 15) >> 2), z = v_swizzle<D>(rsub);
+#pragma unroll
+    for (int dt = 0; dt < kND; ++dt) v_off[dt] = rsub * D + 8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ z) + 4 * (lane & 1);
+  }
+
+  // ---- the wave's query rows through a quarter of the buffers that are filled last, K's and V's second ones, beside tile 0
+  u16* const q_strip = (wave < 2 ? lds_k + S::kTile : lds_v + S::kTile) + (wave & 1) * 32 * D;
+  {
+    const int rows = min(32, n - q0);
+    const u16* const at = q_rows + (long long)q0 * a.q_token;
+    const unsigned long long base = (unsigned long long)at;
+    const u32x4 buffer = {(unsigned)base, (unsigned)(base >> 32) & 0xFFFFu, rows > 0 ? (unsigned)(rows - 1) * a.q_bytes + 2u * D : 0u, 0x00020000u};
+    const unsigned to = lds_at + 2u * (unsigned)(q_strip - lds_k);
+#pragma unroll
+    for (int j = 0; j < 2 * S::kLoads; ++j) {
+      const int row = S::kRowsPerLoad * j + ld_sub;
+      const unsigned of = (unsigned)row * a.q_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks));
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of), "s"(buffer), "s"(to + 1024u * j) : "m0", "memory");
+    }
+  }
+  Feed k_feed{(unsigned long long)k_rows, kTileKeys * a.k_bytes, a.k_bytes, rows_end};
+  Feed v_feed{(unsigned long long)v_rows, kTileKeys * a.v_bytes, a.v_bytes, rows_end};
+  load_tile(k_feed, k_lane, lds_dst(lds_k));
+  load_tile(v_feed, v_lane, lds_dst(lds_v));
+  move_on(k_feed);
+  move_on(v_feed);
+
+  bf16x8 qf[kNK];                        // second operand: Q[q0 + l32][16 s + 8 g .. + 7]
+  f32x16 o[kND], sx, sy;
+  unsigned px[8], py[8];
+  float m_ref = -INFINITY, l_run = 0.f;
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) px[r] = py[r] = 0u;
+  wait_all_but(std::integral_constant<int, S::kLoads>{});              // V(0) may still be on its way
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(q_strip + k_off[st]);
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) asm volatile("" : "+v"(qf[st]));    // read, before the strip is filled again
+  __syncthreads();
+  load_tile(k_feed, k_lane, lds_dst(lds_k + S::kTile));                // K(1)
+  move_on(k_feed);
+  sx = zero;
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) sx = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_b128(lds_k + k_off[st]), qf[st], sx, 0, 0, 0);
+  // (a vector instruction may read a product 12 wait states after it, which the compiler does not see to in another basic block)
+  asm volatile("s_nop 7\n\ts_nop 7" : "+v"(sx));
+
+  // Hides keys that a row does not see; the first block's maximum becomes the row's reference.
+  auto prepare = [&](f32x16& s, int kb, auto mask, auto reference) __attribute__((always_inline)) {
+    if constexpr (decltype(mask)::value) {
+      const int lim = q0 + l32 - kb - 4 * g;       // key kb + 8 (r / 4) + 4 g + r % 4
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = (8 * (r >> 2) + (r & 3) <= lim) ? s[r] : -INFINITY;
+    }
+    if constexpr (decltype(reference)::value) {
+      float v = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) v = fmaxf(v, s[r]);
+      m_ref = max_with_other_half(v);
+    }
+  };
+
+  // One phase, one basic block: every MFMA is followed by its share of the exponentials of the block computed in the phase before, and LDS
+  // reads run kAhead fragments ahead.  Written in the order in which it should issue, with a scheduling fence after every share.  The
+  // work on an element is a chain (scale and shift, exponential, sum, pack), which is skewed over the MFMAs so that no instruction needs the result of the one
+  // before it.
+  //   s_exp -> p_out   P = exp2((S - m) * scale);   s_new = S^T of the next block;   O += P_pend V (kValues)
+  constexpr int kAhead = D / 32;
+  bf16x8 first[kAhead];                            // the first K fragments of a phase 1, read at the end of the phase before it
+  auto phase = [&](const f32x16& s_exp, unsigned (&p_out)[8], f32x16& s_new, const u16* kt, const unsigned (&p_pend)[8], const u16* vt, auto have,
+                   auto values, auto next, const u16* next_kt, auto&& after_mfma) __attribute__((always_inline)) {
+    constexpr bool kHave = decltype(have)::value, kValues = decltype(values)::value, kNext = decltype(next)::value;
+    constexpr int kMfmas = kNK + (kValues ? kNV : 0);
+    const float neg = m_ref == -INFINITY ? 0.f : -m_ref * sl2;
+    float sum = 0.f;
+    bf16x8 kfr[kNK], vfr[kNV];
+    auto read_v = [&](int vi) __attribute__((always_inline)) { vfr[vi] = lds_read_vt(vt + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D); };
+    int ei = 0;
+    float arg = __builtin_fmaf(s_exp[0], sl2, neg), pe1 = 0.f, pe2 = 0.f;
+    auto finish_element = [&](int e) __attribute__((always_inline)) {
+      sum += pe1;
+      asm volatile("" : "+v"(sum));          // (left alone the compiler gathers the additions of several phases in one place)
+      if (e & 1) p_out[e >> 1] = pack_bf16(pe2, pe1);
+    };
+    auto share = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (; ei < 16 * (i + 1) / kMfmas; ++ei) {
+        const float pe = __builtin_amdgcn_exp2f(arg);
+        if (ei + 1 < 16) arg = __builtin_fmaf(s_exp[ei + 1], sl2, neg);
+        if (ei >= 1) finish_element(ei - 1);
+        pe2 = pe1;
+        pe1 = pe;
+      }
+    };
+#pragma unroll
+    for (int st = 0; st < kAhead; ++st) {
+      if constexpr (kHave) kfr[st] = first[st];
+      else kfr[st] = lds_read_b128(kt + k_off[st]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int st = 0; st < kNK; ++st) {
+      if (st + kAhead < kNK) kfr[st + kAhead] = lds_read_b128(kt + k_off[st + kAhead]);
+      else if constexpr (kValues) read_v(st + kAhead - kNK);
+      s_new = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfr[st], qf[st], st == 0 ? zero : s_new, 0, 0, 0);
+      share(st);
+      after_mfma(std::integral_constant<int, 0>{}, st);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (kValues) {
+#pragma unroll
+      for (int vi = 0; vi < kNV; ++vi) {
+        if (vi + kAhead < kNV) read_v(vi + kAhead);
+        else if constexpr (kNext) first[vi + kAhead - kNV] = lds_read_b128(next_kt + k_off[vi + kAhead - kNV]);
+        const int mm = vi % 2;
+        const u32x4 pw = {p_pend[4 * mm], p_pend[4 * mm + 1], p_pend[4 * mm + 2], p_pend[4 * mm + 3]};
+        o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[vi], __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
+        share(kNK + vi);
+        after_mfma(std::integral_constant<int, 1>{}, vi);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    finish_element(15);
+    l_run += sum;
+  };
+
+  typedef std::true_type Yes;
+  typedef std::false_type No;
+  // kTag: t & 1 where the compiler knows it, else -1.  kStart: tile 0, which has no values to add yet and gives the rows their reference.
+  auto body = [&](int t, auto buf_tag, auto start, auto mask) __attribute__((always_inline)) {
+    constexpr int kTag = decltype(buf_tag)::value;
+    constexpr bool kStart = decltype(start)::value;
+    const int buf = kTag >= 0 ? kTag : (t & 1);
+    u16* const k_cur = lds_k + buf * S::kTile;
+    u16* const k_nxt = lds_k + (buf ^ 1) * S::kTile;
+    u16* const v_cur = lds_v + buf * S::kTile;
+    u16* const v_prv = lds_v + (buf ^ 1) * S::kTile;
+    const int kb = t * kTileKeys;
+    prepare(sx, kb, mask, start);
+    phase(sx, px, sy, k_cur + 32 * D, py, v_prv + 32 * D, std::integral_constant<bool, !kStart>{}, std::integral_constant<bool, !kStart>{}, No{}, nullptr,
+          [](auto, int) {});
+    // P_X is due here, in the shadow of this phase's products
+#pragma unroll
+    for (int r = 0; r < 8; ++r) asm volatile("" ::"v"(px[r]));
+    __builtin_amdgcn_sched_barrier(0);
+    wait_all_but(None{});              // the loads that this wave issued in the last phase 2 have landed
+    __syncthreads();
+    prepare(sy, kb + 32, mask, No{});
+    constexpr int kEvery = kNK / S::kLoads;
+    const unsigned k_to = lds_dst(k_cur), v_to = lds_dst(v_prv);
+    phase(sy, py, sx, k_nxt, px, v_cur, No{}, Yes{}, Yes{}, k_nxt + 32 * D, [&](auto half, int i) __attribute__((always_inline)) {
+      if (i % kEvery != 0) return;
+      auto load = [&](auto which) __attribute__((always_inline)) {
+        if constexpr (decltype(half)::value == 0) load_fed(k_feed, k_lane, which, k_to);
+        else load_fed(v_feed, v_lane, which, v_to);
+      };
+      switch (i / kEvery) {
+        case 0: load(std::integral_constant<int, 0>{}); break;
+        case 1: load(std::integral_constant<int, 1>{}); break;
+        case 2: if constexpr (S::kLoads == 4) load(std::integral_constant<int, 2>{}); break;
+        default: if constexpr (S::kLoads == 4) load(std::integral_constant<int, 3>{}); break;
+      }
+    });
+    move_on(k_feed);
+    move_on(v_feed);
+  };
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  typedef std::integral_constant<int, -1> Any;
+  int t = 0;
+  if (my_tiles > 0) {
+    if (n_plain > 0) body(0, Even{}, Yes{}, No{});
+    else body(0, Even{}, Yes{}, Yes{});
+    for (t = 1; t + 1 < n_plain; t += 2) {
+      body(t, Odd{}, No{}, No{});
+      body(t + 1, Even{}, No{}, No{});
+    }
+    for (; t < my_tiles; ++t) body(t, Any{}, No{}, Yes{});       // (a mask does nothing to a tile that is seen whole)
+    // O += P_Y V of the last tile: its V is there since the barrier inside the last body, until the next one
+    const u16* const vt = lds_v + ((my_tiles + 1) & 1) * S::kTile + 32 * D;
+#pragma unroll
+    for (int vi = 0; vi < kNV; ++vi) {
+      const u32x4 pw = {py[4 * (vi % 2)], py[4 * (vi % 2) + 1], py[4 * (vi % 2) + 2], py[4 * (vi % 2) + 3]};
+      o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_vt(vt + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D), __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
+    }
+  }
+  // tiles that only later rows of the workgroup see: in step with their waves
+  for (; t < n_tiles; ++t) {
+    wait_all_but(None{});
+    __syncthreads();
+    load_tile(k_feed, k_lane, lds_dst(lds_k + (t & 1) * S::kTile));
+    load_tile(v_feed, v_lane, lds_dst(lds_v + ((t & 1) ^ 1) * S::kTile));
+    move_on(k_feed);
+    move_on(v_feed);
+  }
+  wait_all_but(None{});
+  __syncthreads();               // nothing is on its way into LDS, and nobody reads a tile any more
+  if (q0 >= n) return;
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[dt]));
+
+  float l_row = sum_with_other_half(l_run);
+  // what is not finite is not 0 when it is multiplied by 0
+  float check = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[dt][r], 0.f, check);
+  if (__any(!(l_row <= 0x1p64f) || !(check == 0.f))) {
+    // ---- the slow way: running maximum, one block of 32 keys at a time straight from memory
+    float m_run = -INFINITY;
+    l_row = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
+    for (int kb = 0; kb < min(n, q0 + 32); kb += 32) {
+      f32x16 s = zero;
+      const u16* const kr = k_rows + (long long)min(kb + l32, n - 1) * a.k_token + 8 * g;
+#pragma unroll
+      for (int st = 0; st < kNK; ++st)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kr + 16 * st)), qf[st], s, 0, 0, 0);
+      const int lim = q0 + l32 - kb - 4 * g;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = (8 * (r >> 2) + (r & 3) <= lim) ? s[r] : -INFINITY;
+        mx = fmaxf(mx, s[r]);
+      }
+      const float m_new = fmaxf(m_run, max_with_other_half(mx)), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run - m_use) * sl2), neg = -m_use * sl2;
+      m_run = m_new;
+      l_row *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < kND; ++dt) o[dt] *= alpha;
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sl2, neg));
+        sum += s[r];
+      }
+      l_row += sum_with_other_half(sum);
+      // key by key; key 8 (r / 4) + 4 half + r % 4 is in register r of the lanes of that half
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = kb + 8 * (r >> 2) + 4 * half + (r & 3);
+          const float mine = s[r], others = __shfl_xor(mine, 32), p = g == half ? mine : others;
+          const u16* const vr = v_rows + (long long)min(key, n - 1) * a.v_token + 4 * g;
+          const bool seen = key <= q0 + l32;
+#pragma unroll
+          for (int dt = 0; dt < kND; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const u32x2 w = *reinterpret_cast<const u32x2*>(vr + 32 * dt + 8 * j);
+              const float v[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[dt][4 * j + e] = seen ? __builtin_fmaf(p, v[e], o[dt][4 * j + e]) : o[dt][4 * j + e];
+            }
+        }
+    }
+  }
+
+  // ---- rows to memory, through this wave's strip of LDS so that the stores are whole rows
+  const float inv = 1.f / l_row;
+  u32x4* const rows = reinterpret_cast<u32x4*>(lds_raw) + wave * 32 * S::kChunks;
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {        // fours j of a channel tile are its channels 8 j + 4 g .. + 3: the halves of the wave exchange one of two
+      const f32x16& x = o[dt];
+      const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j] * inv, x[4 * j + 1] * inv), pack_bf16(x[4 * j + 4] * inv, x[4 * j + 5] * inv), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j + 2] * inv, x[4 * j + 3] * inv), pack_bf16(x[4 * j + 6] * inv, x[4 * j + 7] * inv), false, false);
+      rows[l32 * S::kChunks + ((4 * dt + j + g) ^ (l32 % S::kChunks))] = u32x4{lo[0], hi[0], lo[1], hi[1]};
+    }
+#pragma unroll
+  for (int it = 0; it < S::kChunks / 2; ++it) {
+    const int r = (64 * it + lane) / S::kChunks, ch = lane % S::kChunks;
+    const u32x4 val = rows[r * S::kChunks + (ch ^ (r % S::kChunks))];
+    if (q0 + r < n) *reinterpret_cast<u32x4*>(out_rows + (long long)(q0 + r) * a.out_token + 8 * ch) = val;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) {
+  const dim3 grid(a.workgroups);
+  if (head_dim == 128) hipLaunchKernelGGL(prompt_kernel<128>, grid, dim3(kThreads), Shape<128>::kLds, s, a);
+  else hipLaunchKernelGGL(prompt_kernel<64>, grid, dim3(kThreads), Shape<64>::kLds, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace kvp

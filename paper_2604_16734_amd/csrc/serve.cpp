@@ -123,4 +123,38 @@ int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* s
   return page_rows(pages, rows, seq_begin, table, table_width, first, n_seqs, stream, false);
 }
 
+int kvp_prompt_attention(const kvp_prompts* p, void* stream) {
+  if (!p || !valid_group(p->n_q_heads, p->n_kv_heads) || (p->head_dim != 64 && p->head_dim != 128)) return KVP_EINVAL;
+  if (p->n_tokens < 0 || p->n_seqs < 1 || p->n_seqs > KVP_MAX_SEQUENCES || !aligned(p->seq_begin, 4) || !valid_scale(p->softmax_scale)) return KVP_EINVAL;
+  const int64_t strides[4][2] = {{p->q_token, p->q_head}, {p->k_token, p->k_head}, {p->v_token, p->v_head}, {p->out_token, p->out_head}};
+  for (const auto& s : strides)
+    if (!valid_strides(s[0], s[1]) || (p->n_tokens > 1 && s[0] < p->head_dim)) return KVP_EINVAL;
+  if (!separate_rows(p->out_token, p->out_head, p->n_tokens, p->n_q_heads, p->head_dim)) return KVP_EINVAL;
+  // tiles of rows, at most: every prompt may have one that is not full
+  const long long tiles = (long long)p->n_tokens / kPromptRows + p->n_seqs;
+  if (tiles * p->n_q_heads > 1ll << 30) return KVP_EINVAL;
+  if (p->n_tokens == 0) return KVP_OK;
+  if (!aligned(p->q, 16) || !aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->out, 16)) return KVP_EINVAL;
+  PromptArgs a{};
+  a.q = static_cast<const u16*>(p->q);
+  a.k = static_cast<const u16*>(p->k);
+  a.v = static_cast<const u16*>(p->v);
+  a.out = static_cast<u16*>(p->out);
+  a.seq_begin = p->seq_begin;
+  a.q_token = p->q_token; a.q_head = p->q_head;
+  a.k_token = p->k_token; a.k_head = p->k_head;
+  a.v_token = p->v_token; a.v_head = p->v_head;
+  a.out_token = p->out_token; a.out_head = p->out_head;
+  // (of one row the distance to the next means nothing; the kernel's addresses count on one)
+  auto bytes = [&](int64_t token) { return 2u * (unsigned)(token < p->head_dim ? p->head_dim : token); };
+  a.q_bytes = bytes(p->q_token); a.k_bytes = bytes(p->k_token); a.v_bytes = bytes(p->v_token);
+  a.n_tokens = p->n_tokens; a.n_seqs = p->n_seqs; a.n_q_heads = p->n_q_heads;
+  a.heads_per_xcd = p->n_q_heads % kXcds == 0 ? p->n_q_heads / kXcds : 0;
+  a.workgroups = (unsigned)(tiles * p->n_q_heads);
+  a.by_heads = divisor_of((unsigned)(a.heads_per_xcd ? a.heads_per_xcd : p->n_q_heads), a.workgroups);
+  a.by_group = divisor_of((unsigned)(p->n_q_heads / p->n_kv_heads), (unsigned)p->n_q_heads);
+  a.scale_log2 = scale_log2_of(p->softmax_scale, p->head_dim);
+  return code_of(launch_prompt(a, p->head_dim, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

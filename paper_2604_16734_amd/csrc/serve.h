@@ -41,6 +41,24 @@ struct PagedDecodeArgs {
 int paged_decode_workgroups(int head_dim, bool e4m3);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);
 
+constexpr int kPromptRows = 128;       // query rows of a workgroup
+struct PromptArgs {
+  const u16* q;
+  const u16* k;
+  const u16* v;
+  u16* out;
+  const int32_t* seq_begin;
+  long long q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  unsigned q_bytes, k_bytes, v_bytes;      // from token to token
+  int n_tokens, n_seqs, n_q_heads;
+  int heads_per_xcd;          // 0: the heads cannot be dealt out evenly
+  unsigned workgroups;
+  Divisor by_heads;           // heads_per_xcd, or n_q_heads
+  Divisor by_group;
+  float scale_log2;
+};
+hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s);
+
 hipError_t launch_page_write(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
 hipError_t launch_page_read(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
 

@@ -3,7 +3,7 @@ once with torch tensors as their arguments.  Marshalling only, as in binding.py.
 import contextlib
 import ctypes
 
-from .binding import (KVP_EINVAL, KVP_PAGE_BF16, KVP_PAGE_E4M3, KvpError, KvpPages, KvpRows, lib)
+from .binding import KVP_EINVAL, KVP_PAGE_BF16, KVP_PAGE_E4M3, KvpError, KvpPages, KvpPrompts, KvpRows, lib
 
 
 def _need(ok, what):
@@ -56,6 +56,28 @@ def _whole(t, shape, device, what):
     import torch
     _need(t.dtype is torch.int32 and t.device == device and t.shape == shape and t.is_contiguous(), what)
     return t.data_ptr()
+
+
+def prompt_attention(q, k, v, seq_begin, out=None, softmax_scale=0.0, stream=None):
+    """Causal attention inside each of the prompts whose rows are seq_begin[s] .. seq_begin[s + 1] - 1 of q [n_tokens, n_q_heads, d] and
+    of k and v [n_tokens, n_kv_heads, d], any strides but the last (kvp_prompt_attention).  Rows behind the last prompt are left as they
+    were in `out`; without one given they hold whatever was there."""
+    import torch
+    what, device = "prompt_attention: ", q.device
+    _need(q.dim() == 3 and k.dim() == 3 and device.type == "cuda" and device.index is not None, what + "q and k")
+    (n_tokens, n_q_heads, d), n_kv_heads, n_seqs = q.shape, k.shape[1], seq_begin.numel() - 1
+    at = [_numbers(q, (n_tokens, n_q_heads, d), device, what + "q")]
+    at += [_numbers(t, (n_tokens, n_kv_heads, d), device, what + "k and v") for t in (k, v)]
+    begin = _whole(seq_begin, (n_seqs + 1,), device, what + "seq_begin")
+    with _On(device, stream) as handle:
+        if out is None:
+            out = torch.empty((n_tokens, n_q_heads, d), dtype=torch.bfloat16, device=device)
+        at.append(_numbers(out, (n_tokens, n_q_heads, d), device, what + "out"))
+        prompts = KvpPrompts(*(x[0] for x in at), begin, *(s for x in at for s in x[1:]), n_tokens, n_seqs, n_q_heads, n_kv_heads, d, softmax_scale)
+        rc = lib().kvp_prompt_attention(ctypes.byref(prompts), handle)
+    if rc:
+        raise KvpError(rc, "kvp_prompt_attention")
+    return out
 
 
 class Pages:
