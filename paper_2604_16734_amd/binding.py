@@ -178,14 +178,14 @@ class _Entries:
 _entries = _Entries()
 
 
-def _fast_call():
-    """csrc/fast_calls.cpp's call, where it has been built for this Python (by its file's name) and this torch."""
+def _fast_call(name="call"):
+    """A function of csrc/fast_calls.cpp, where it has been built for this Python (by its file's name) and this torch."""
     import torch
     try:
         from . import _fast_calls
     except ImportError:
         return _not_taken
-    return _fast_calls.call if getattr(_fast_calls, "torch_version", None) == str(torch.__version__) else _not_taken
+    return getattr(_fast_calls, name, _not_taken) if getattr(_fast_calls, "torch_version", None) == str(torch.__version__) else _not_taken
 
 
 def _segments(segs):

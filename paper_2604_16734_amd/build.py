@@ -48,7 +48,7 @@ def build_fast_calls(out=FAST_CALLS, defines=()):
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
     cmd += ["-D" + d for d in ('KVP_TORCH_VERSION="%s"' % torch.__version__,) + tuple(defines)]
-    cmd += ["-I" + d for d in include_paths() + [sysconfig.get_paths()["include"]]]
+    cmd += ["-I" + os.path.join(ROOT, "include")] + ["-I" + d for d in include_paths() + [sysconfig.get_paths()["include"]]]
     cmd += [os.path.join(CSRC, "fast_calls.cpp"), "-o", out, "-L" + torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10",
             "-Wl,-rpath," + torch_lib]
     _run(cmd)

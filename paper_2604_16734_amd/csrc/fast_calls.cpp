@@ -1,16 +1,19 @@
-// The per-layer calls of Cache (binding.py) from Python without ctypes: a module of one function, which looks at the tensors and
-// calls the C entry point.  A decode step of a small cache takes the GPU less than the checks and conversions of the same call took
+// The per-layer calls of Cache (binding.py) and those of pages.py from Python without ctypes: functions that look at the tensors and
+// call the C entry point.  A decode step of a small cache takes the GPU less than the checks and conversions of the same call took
 // in Python.
 //
 // call(entry, handle, layer, tensors, q_row, kv_row, device, stream, token_begin) -> the entry point's code, or None where anything
 // about the arguments is not plainly as it should be: the caller then takes its Python path, which has the same checks and says what is
-// wrong.  Nothing is kept from one call to the next, and no C++ exception leaves: what a tensor throws when it is looked at counts as not plain.
+// wrong.  page_rows, paged_decode and prompt (below) likewise.  Nothing is kept from one call to the next, and no C++ exception leaves: what a tensor throws when it is looked at counts as not plain.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+
+#include "kvp.h"
 
 // where the tensors have to be (the tests build the module for the CPU, too)
 #ifndef KVP_TENSOR_DEVICE
@@ -21,8 +24,8 @@ namespace {
 
 constexpr int kMostTensors = 5;
 
-// a plain contiguous bf16 tensor of `device`; its address is then what data_ptr() gives
-bool plain(PyObject* o, int64_t device, const at::Tensor** out) {
+// a plain tensor of `device` and of this type; its address is then what data_ptr() gives
+bool plain_of(PyObject* o, int64_t device, at::ScalarType type, const at::Tensor** out) {
   if (!THPVariable_CheckExact(o)) return false;
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || t.is_nested()) return false;
@@ -30,12 +33,14 @@ bool plain(PyObject* o, int64_t device, const at::Tensor** out) {
   if (keys.has_any(c10::DispatchKeySet({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
                                         c10::DispatchKey::Functionalize, c10::DispatchKey::Batched, c10::DispatchKey::ZeroTensor})))
     return false;
-  if (t.layout() != at::kStrided || !t.has_storage() || t.scalar_type() != at::kBFloat16 || !t.is_contiguous()) return false;
+  if (t.layout() != at::kStrided || !t.has_storage() || t.scalar_type() != type) return false;
   const c10::Device d = t.device();
   if (d.type() != KVP_TENSOR_DEVICE || d.index() != device) return false;
   *out = &t;
   return true;
 }
+// a contiguous one of bf16
+bool plain(PyObject* o, int64_t device, const at::Tensor** out) { return plain_of(o, device, at::kBFloat16, out) && (*out)->is_contiguous(); }
 
 bool small_int(PyObject* o, int32_t* out) {
   if (!PyLong_CheckExact(o)) return false;
@@ -128,7 +133,137 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   return PyLong_FromLong(code);
 }
 
-PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
+// ---- the calls of many sequences
+struct Numbers {                  // bf16 rows [tokens, heads, d]
+  void* at;
+  int64_t token, head;
+};
+bool numbers(PyObject* o, int64_t device, int64_t tokens, int64_t heads, int64_t d, Numbers* out) {
+  const at::Tensor* t;
+  if (!plain_of(o, device, at::kBFloat16, &t) || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads || t->size(2) != d || t->stride(2) != 1) return false;
+  *out = Numbers{t->numel() > 0 ? t->mutable_data_ptr() : nullptr, tokens > 1 ? t->stride(0) : 0, heads > 1 ? t->stride(1) : 0};
+  return true;
+}
+// contiguous int32 numbers
+bool whole(PyObject* o, int64_t device, const at::Tensor** out) { return plain_of(o, device, at::kInt, out) && (*out)->is_contiguous(); }
+const int32_t* ints(const at::Tensor* t) { return t->numel() > 0 ? static_cast<const int32_t*>(t->const_data_ptr()) : nullptr; }
+
+// page_rows(entry, pages, n_kv_heads, head_dim, device, stream, k, v, seq_begin, table, first)
+PyObject* page_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (n_args != 11) {
+    PyErr_SetString(PyExc_TypeError, "page_rows takes eleven arguments");
+    return nullptr;
+  }
+  void *entry, *pages, *stream;
+  int32_t heads, d, device;
+  if (!address(args[0], &entry) || !entry || !address(args[1], &pages) || !pages || !small_int(args[2], &heads) || !small_int(args[3], &d) ||
+      !small_int(args[4], &device) || !address(args[5], &stream))
+    Py_RETURN_NONE;
+  kvp_rows rows;
+  const at::Tensor *begin, *table, *first = nullptr;
+  int32_t n_seqs, width;
+  try {
+    const at::Tensor* k;
+    Numbers kn, vn;
+    if (!plain_of(args[6], device, at::kBFloat16, &k) || k->dim() != 3 || k->size(0) > INT32_MAX) Py_RETURN_NONE;
+    const int64_t n = k->size(0);
+    if (!numbers(args[6], device, n, heads, d, &kn) || !numbers(args[7], device, n, heads, d, &vn)) Py_RETURN_NONE;
+    if (!whole(args[8], device, &begin) || !whole(args[9], device, &table) || begin->dim() != 1 || table->dim() != 2) Py_RETURN_NONE;
+    if (begin->size(0) > INT32_MAX || table->size(0) != begin->size(0) - 1 || table->size(1) > INT32_MAX) Py_RETURN_NONE;
+    if (args[10] != Py_None && (!whole(args[10], device, &first) || first->dim() != 1 || first->size(0) != table->size(0))) Py_RETURN_NONE;
+    rows = kvp_rows{kn.at, vn.at, kn.token, kn.head, vn.token, vn.head, (int32_t)n};
+    n_seqs = (int32_t)table->size(0);
+    width = (int32_t)table->size(1);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  int code;
+  Py_BEGIN_ALLOW_THREADS;
+  code = ((decltype(&kvp_page_write))entry)((const kvp_pages*)pages, &rows, ints(begin), ints(table), width, first ? ints(first) : nullptr, n_seqs, stream);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(code);
+}
+
+// paged_decode(entry, pages, n_q_heads, head_dim, device, stream, q, table, lengths, out, workspace or its bytes, softmax_scale).  With a number of
+// bytes the workspace is allocated here, for the stream that torch works on.
+PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (n_args != 12) {
+    PyErr_SetString(PyExc_TypeError, "paged_decode takes twelve arguments");
+    return nullptr;
+  }
+  void *entry, *pages, *stream;
+  int32_t heads, d, device, bytes = 0;
+  if (!address(args[0], &entry) || !entry || !address(args[1], &pages) || !pages || !small_int(args[2], &heads) || !small_int(args[3], &d) ||
+      !small_int(args[4], &device) || !address(args[5], &stream) || !PyFloat_CheckExact(args[11]))
+    Py_RETURN_NONE;
+  const bool own = small_int(args[10], &bytes);
+  const at::Tensor *table, *lengths, *out, *room;
+  at::Tensor made;
+  Numbers q;
+  int32_t n_seqs, width;
+  try {
+    if (!whole(args[7], device, &table) || !whole(args[8], device, &lengths) || table->dim() != 2 || lengths->dim() != 1) Py_RETURN_NONE;
+    if (lengths->size(0) > INT32_MAX || table->size(0) != lengths->size(0) || table->size(1) > INT32_MAX) Py_RETURN_NONE;
+    n_seqs = (int32_t)lengths->size(0);
+    width = (int32_t)table->size(1);
+    if (!numbers(args[6], device, n_seqs, heads, d, &q) || !plain(args[9], device, &out)) Py_RETURN_NONE;
+    if (out->dim() != 3 || out->size(0) != n_seqs || out->size(1) != heads || out->size(2) != d) Py_RETURN_NONE;
+    if (own) {
+      made = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(c10::Device(KVP_TENSOR_DEVICE, (c10::DeviceIndex)device)));
+      room = &made;
+    } else if (!plain_of(args[10], device, at::kByte, &room) || !room->is_contiguous()) {
+      Py_RETURN_NONE;
+    }
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  int code;
+  const float scale = (float)PyFloat_AS_DOUBLE(args[11]);
+  Py_BEGIN_ALLOW_THREADS;
+  code = ((decltype(&kvp_paged_decode))entry)((const kvp_pages*)pages, q.at, q.token, q.head, heads, ints(table), width, ints(lengths), n_seqs, scale,
+                                              out->numel() > 0 ? out->mutable_data_ptr() : nullptr,
+                                              room->numel() > 0 ? room->mutable_data_ptr() : nullptr, (size_t)room->numel(), stream);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(code);
+}
+
+// prompt(entry, device, stream, q, k, v, seq_begin, out, softmax_scale)
+PyObject* prompt(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (n_args != 9) {
+    PyErr_SetString(PyExc_TypeError, "prompt takes nine arguments");
+    return nullptr;
+  }
+  void *entry, *stream;
+  int32_t device;
+  if (!address(args[0], &entry) || !entry || !small_int(args[1], &device) || !address(args[2], &stream) || !PyFloat_CheckExact(args[8])) Py_RETURN_NONE;
+  kvp_prompts p;
+  try {
+    const at::Tensor *qt, *kt, *begin;
+    Numbers q, k, v, out;
+    if (!plain_of(args[3], device, at::kBFloat16, &qt) || !plain_of(args[4], device, at::kBFloat16, &kt) || qt->dim() != 3 || kt->dim() != 3) Py_RETURN_NONE;
+    const int64_t n = qt->size(0), hq = qt->size(1), d = qt->size(2), hkv = kt->size(1);
+    if (n > INT32_MAX || hq > INT32_MAX || hkv > INT32_MAX || d > INT32_MAX) Py_RETURN_NONE;
+    if (!numbers(args[3], device, n, hq, d, &q) || !numbers(args[4], device, n, hkv, d, &k) || !numbers(args[5], device, n, hkv, d, &v) ||
+        !numbers(args[7], device, n, hq, d, &out))
+      Py_RETURN_NONE;
+    if (!whole(args[6], device, &begin) || begin->dim() != 1 || begin->size(0) < 1 || begin->size(0) > INT32_MAX) Py_RETURN_NONE;
+    p = kvp_prompts{q.at, k.at, v.at, out.at, ints(begin), q.token, q.head, k.token, k.head, v.token, v.head, out.token, out.head,
+                    (int32_t)n, (int32_t)(begin->size(0) - 1), (int32_t)hq, (int32_t)hkv, (int32_t)d, (float)PyFloat_AS_DOUBLE(args[8])};
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  int code;
+  Py_BEGIN_ALLOW_THREADS;
+  code = ((decltype(&kvp_prompt_attention))entry)(&p, stream);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(code);
+}
+
+#define KVP_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {KVP_METHOD(call), KVP_METHOD(page_rows), KVP_METHOD(paged_decode), KVP_METHOD(prompt), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -65,6 +65,25 @@ __device__ __forceinline__ float over_rows(float x, Op op, bool eight_lanes) {  
 struct FloatMax { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct FloatSum { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 
+template <class Op>
+__device__ __forceinline__ float over_wave(float x, Op op) {      // over all lanes, in all lanes
+  x = op(x, dpp_lane<0xB1>(x));
+  x = op(x, dpp_lane<0x4E>(x));
+  x = op(x, dpp_lane<0x141>(x));
+  return over_rows(x, op, true);
+}
+// Sum over the lanes of a wave up to and with this one; the last lane has the sum of all.
+__device__ __forceinline__ int sum_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);      // the lane 1, 2, 4, 8 before it, among sixteen
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // the last lane of the sixteen before, of the 32 before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+__device__ __forceinline__ int sum_of_wave(int x) { return __builtin_amdgcn_readlane(sum_upto(x), 63); }
+
 // Sums of v[0 .. N - 1] over the rows of a wave; lanes 16 r .. 16 r + 15 (r = 0 .. 3) end up with those of
 // v[r N / 4 .. (r + 1) N / 4 - 1], in v[0 .. N / 4 - 1].
 template <int kPieces, int N>

@@ -84,21 +84,8 @@ __device__ __forceinline__ bf16x8 lds_read_vt16(const unsigned char* p, int rows
 __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, int seq) {
   return seq < a.n_seqs ? min(max(a.lengths[seq], 0), a.width << a.pool.shift) : 0;
 }
-__device__ __forceinline__ unsigned sum_of_wave(unsigned x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += (unsigned)__shfl_xor((int)x, d);
-  return x;
-}
-__device__ __forceinline__ unsigned sum_before(unsigned x, int lane) {       // of the lanes up to and with this one
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const unsigned y = (unsigned)__shfl_up((int)x, d);
-    x += lane >= d ? y : 0u;
-  }
-  return x;
-}
-
-template <int D, bool kE4m3>
+// kDirect: workgroup b has all of sequence b / n_heads, KV head b % n_heads, and there is nothing to join.
+template <int D, bool kE4m3, bool kDirect>
 __global__ void __launch_bounds__(kThreads, (Shape<D, kE4m3>::kPerCu * kWaves / 4))
 paged_decode_kernel(const PagedDecodeArgs a) {
   using S = Shape<D, kE4m3>;
@@ -110,23 +97,41 @@ paged_decode_kernel(const PagedDecodeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // ---- this workgroup's share, and the sequence that it begins in
-  unsigned mine = 0;
-  for (int s = lane; s < a.n_seqs; s += 64) mine += (unsigned)paged_tiles(length_of(a, s));
-  const unsigned units = (unsigned)__builtin_amdgcn_readfirstlane(sum_of_wave(mine)) * (unsigned)a.pool.n_heads;
-  const unsigned share = (unsigned)__builtin_amdgcn_readfirstlane(paged_share(units, (unsigned)a.workgroups));
-  unsigned at = blockIdx.x * share;
-  if (at >= units) return;
-  const unsigned end = min(units, at + share);
-  // of 64 sequences at a time: lengths, and the units before each
-  int group0 = 0, length = length_of(a, lane);
-  unsigned before = 0, tiles = (unsigned)paged_tiles(length) * (unsigned)a.pool.n_heads, upto = sum_before(tiles, lane);
-  auto next_group = [&]() __attribute__((always_inline)) {
-    before += (unsigned)__builtin_amdgcn_readlane(upto, 63);
-    group0 += 64;
+  unsigned at = 0, end = 1, share = 1;
+  int seq = -1, n_keys = 0, direct_head = 0, ids = -1;
+  // of 64 sequences at a time: lengths, and the units up to each
+  int group0 = 0, length = 0;
+  unsigned before = 0, tiles = 0, upto = 0;
+  auto next_group = [&](int from) __attribute__((always_inline)) {
+    before += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    group0 = from;
     length = length_of(a, group0 + lane);
     tiles = (unsigned)paged_tiles(length) * (unsigned)a.pool.n_heads;
-    upto = sum_before(tiles, lane);
+    upto = (unsigned)sum_upto((int)tiles);
   };
+  if constexpr (kDirect) {
+    seq = (int)quotient(blockIdx.x, a.by_heads);
+    direct_head = (int)blockIdx.x - seq * a.pool.n_heads;
+    ids = lane < a.width ? a.table[(size_t)seq * a.width + lane] : -1;       // (beside the length, not after it)
+    n_keys = length_of(a, seq);
+    if (n_keys == 0) {
+      for (int i = threadIdx.x; i < a.group * D / 8; i += kThreads)
+        reinterpret_cast<u32x4*>(a.out + ((size_t)seq * a.n_q_heads + direct_head * a.group) * D)[i] = u32x4{0u, 0u, 0u, 0u};
+      return;
+    }
+    ids = ids < a.pool.n_pages ? ids : -1;
+    asm volatile("" : "+v"(ids));
+  } else {
+    next_group(0);
+    int others = 0;
+    for (int s = 64 + lane; s < a.n_seqs; s += 64) others += paged_tiles(length_of(a, s));
+    unsigned units = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    if (a.n_seqs > 64) units += (unsigned)sum_of_wave(others) * (unsigned)a.pool.n_heads;
+    share = (unsigned)__builtin_amdgcn_readfirstlane(paged_share(units, (unsigned)a.workgroups));
+    at = blockIdx.x * share;
+    if (at >= units) return;
+    end = min(units, at + share);
+  }
 
   // ---- LDS: [wave][K strip, V strip, exponents]
   unsigned char* const k_strip = lds + wave * S::kWaveBytes;
@@ -202,25 +207,24 @@ paged_decode_kernel(const PagedDecodeArgs a) {
   const float sl2 = a.scale_log2;
 
   // ---- pieces
-  int seq = -1, n_keys = 0;
   unsigned seq_first = 0, seq_end = 0;
   while (at < end) {
-    if (seq < 0 || at >= seq_end) {               // the sequence of unit `at`
-      while (before + (unsigned)__builtin_amdgcn_readlane(upto, 63) <= at && group0 + 64 < a.n_seqs) next_group();
+    if (!kDirect && (seq < 0 || at >= seq_end)) {               // the sequence of unit `at`
+      while (before + (unsigned)__builtin_amdgcn_readlane((int)upto, 63) <= at && group0 + 64 < a.n_seqs) next_group(group0 + 64);
       const int i = __builtin_ctzll(__ballot(before + upto > at));
       seq = group0 + i;
       n_keys = __builtin_amdgcn_readlane(length, i);
-      seq_end = before + (unsigned)__builtin_amdgcn_readlane(upto, i);
-      seq_first = seq_end - (unsigned)__builtin_amdgcn_readlane(tiles, i);
+      seq_end = before + (unsigned)__builtin_amdgcn_readlane((int)upto, i);
+      seq_first = seq_end - (unsigned)__builtin_amdgcn_readlane((int)tiles, i);
     }
     const unsigned n_tiles = (unsigned)paged_tiles(n_keys);
-    const int head = __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
+    const int head = kDirect ? direct_head : __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
     const unsigned first = seq_first + (unsigned)head * n_tiles;      // the first unit of this sequence and head
-    const int t0 = (int)(at - first), t1 = (int)(min(end, first + n_tiles) - first);
+    const int t0 = kDirect ? 0 : (int)(at - first), t1 = kDirect ? (int)n_tiles : (int)(min(end, first + n_tiles) - first);
     const int32_t* const row_of_table = a.table + (size_t)seq * a.width;
 
     // the page numbers of 64 columns from col0 on; -1: no such page
-    int col0 = 0, ids = -1;
+    int col0 = 0;
     auto load_ids = [&](int col) __attribute__((always_inline)) {
       col0 = col;
       const int id = col + lane < a.width ? row_of_table[col + lane] : -1;
@@ -228,7 +232,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       asm volatile("" : "+v"(ids));               // here, not where it is used: the wait there would be for all loads, every time
     };
     const int kb0 = kPagedTile * t0 + kKeys * wave;
-    if (kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
+    if (!kDirect && kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
 
     // Q: second operand, column l16 of the products; channels in the order of K's fragments
     bf16x8 qf[kSteps];
@@ -404,8 +408,8 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       stat[kHeads + lane] = l;
     }
     __syncthreads();
-    const bool whole = piece_is_whole(first, n_tiles, share);
-    const size_t slot = (size_t)piece_slot(first, blockIdx.x, share) * a.group;
+    const bool whole = kDirect || piece_is_whole(first, n_tiles, share);
+    const size_t slot = kDirect ? 0 : (size_t)piece_slot(first, blockIdx.x, share) * a.group;
 #pragma unroll
     for (int i = 0; i < 64 * kTiles / kThreads; ++i) {
       const int item = kThreads * i + threadIdx.x, column = item % 16, ch = 16 * (item / 64) + 4 * (item / 16 % 4);
@@ -434,76 +438,158 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         }
       }
     }
+    if constexpr (kDirect) return;
     __syncthreads();
     at = first + (unsigned)t1;
   }
 }
 
-// ---- the pieces of one sequence and query head, joined; a sequence without keys has zeros
+// ---- the pieces of one sequence and query head, joined; a sequence without keys has zeros.  First their weights, then the weighted sum, whose
+// loads do not wait for one another.
+struct Pieces {
+  unsigned first, n_tiles, share, w0, n;       // first unit, units; the workgroups that have pieces are w0 .. w0 + n - 1; n = 1: whole
+};
+__device__ __forceinline__ Pieces pieces_of(const PagedDecodeArgs& a, int seq, int head, int lane) {
+  int all = 0, earlier = 0;
+  for (int s = lane; s < a.n_seqs; s += 64) {
+    const int t = paged_tiles(length_of(a, s));
+    all += t;
+    earlier += s < seq ? t : 0;
+  }
+  Pieces p;
+  const unsigned units = (unsigned)sum_of_wave(all) * (unsigned)a.pool.n_heads;
+  p.n_tiles = (unsigned)paged_tiles(length_of(a, seq));
+  p.share = (unsigned)__builtin_amdgcn_readfirstlane((int)paged_share(units, (unsigned)a.workgroups));
+  p.first = (unsigned)sum_of_wave(earlier) * (unsigned)a.pool.n_heads + (unsigned)head * p.n_tiles;
+  p.w0 = (unsigned)__builtin_amdgcn_readfirstlane((int)(p.first / p.share));
+  p.n = p.n_tiles == 0 ? 0u : (unsigned)__builtin_amdgcn_readfirstlane((int)((p.first + p.n_tiles - 1) / p.share)) - p.w0 + 1;
+  return p;
+}
+
+// Many sequences: a wave for each query head of one.  (96 sequences, 32/8 heads, d 128: 15.8 us with the kernel below, 5.0 this way.)
 template <int D>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedDecodeArgs a) {
-  constexpr int kLanes = D / 4, kSlots = kThreads / kLanes;       // lanes of a slot's row; slots at a time
-  __shared__ f32x4 rows[kSlots][kLanes];
-  __shared__ float tops[kSlots], sums[kSlots];
-  const int lane = threadIdx.x & 63, hq = blockIdx.x, seq = blockIdx.y, head = hq / a.group, column = hq - head * a.group;
-  unsigned mine = 0, mine_before = 0;
-  for (int s = lane; s < a.n_seqs; s += 64) {
-    const unsigned t = (unsigned)paged_tiles(length_of(a, s));
-    mine += t;
-    mine_before += s < seq ? t : 0u;
-  }
-  const unsigned units = sum_of_wave(mine) * (unsigned)a.pool.n_heads;
-  const unsigned n_tiles = (unsigned)paged_tiles(length_of(a, seq)), share = paged_share(units, (unsigned)a.workgroups);
-  const unsigned first = sum_of_wave(mine_before) * (unsigned)a.pool.n_heads + (unsigned)head * n_tiles;
-  if (n_tiles > 0 && piece_is_whole(first, n_tiles, share)) return;
-  const int sub = threadIdx.x / kLanes, piece = threadIdx.x % kLanes;
+  constexpr int kLanes = D / 4, kSlots = 64 / kLanes;
+  const int lane = threadIdx.x & 63, seq = blockIdx.y, hq = kWaves * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (hq >= a.n_q_heads) return;
+  const int head = (int)quotient((unsigned)hq, a.by_group), column = hq - head * a.group;
+  const Pieces p = pieces_of(a, seq, head, lane);
+  u16* const out = a.out + ((size_t)seq * a.n_q_heads + hq) * D;
+  if (p.n == 0 && lane < kLanes) reinterpret_cast<u32x2*>(out)[lane] = u32x2{0u, 0u};
+  if (p.n <= 1) return;
+  const float* const stats = a.partial + (size_t)2 * a.workgroups * a.group * D;
+  auto slot_of = [&](unsigned i) __attribute__((always_inline)) { return (size_t)piece_slot(p.first, p.w0 + i, p.share) * a.group + column; };
+  const int sub = lane / kLanes, piece = lane % kLanes;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  if (n_tiles > 0) {
-    const unsigned w1 = (first + n_tiles - 1) / share;
-    for (unsigned w = first / share + (unsigned)sub; w <= w1; w += kSlots) {
-      const size_t slot = (size_t)piece_slot(first, w, share) * a.group + column;
-      const float* const stat = a.partial + (size_t)2 * a.workgroups * a.group * D + 2 * slot;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.partial + slot * D + 4 * piece);
-      const float top = fmaxf(m, stat[0]), use = top == -INFINITY ? 0.f : top;
-      const float f0 = __builtin_amdgcn_exp2f(m - use), f1 = __builtin_amdgcn_exp2f(stat[0] - use);
-      o = o * f0 + x * f1;
-      l = l * f0 + stat[1] * f1;
-      m = top;
+  for (unsigned base = 0; base < p.n; base += 64) {
+    const unsigned here = min(64u, p.n - base);
+    const bool mine = (unsigned)lane < here;
+    const float* const stat = stats + 2 * slot_of(base + (mine ? lane : 0));
+    const float top = mine ? stat[0] : -INFINITY, sum = mine ? stat[1] : 0.f;
+    const float most = fmaxf(m, over_wave(top, FloatMax{})), use = most == -INFINITY ? 0.f : most;
+    const float by = __builtin_amdgcn_exp2f(m - use), f = __builtin_amdgcn_exp2f(top - use);
+    m = most;
+    l = l * by + over_wave(f * sum, FloatSum{});
+    o *= by;
+#pragma unroll 4
+    for (unsigned i = sub; i < (here + kSlots - 1) / kSlots * kSlots; i += kSlots) {      // (all lanes: the last ones again, with weight 0)
+      const float w = __shfl(f, (int)i);
+      o += w * *reinterpret_cast<const f32x4*>(a.partial + slot_of(base + min(i, here - 1)) * D + 4 * piece);
     }
   }
-  rows[sub][piece] = o;
-  if (piece == 0) {
-    tops[sub] = m;
-    sums[sub] = l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x = o[e], y = x;
+    if constexpr (kSlots == 4) {
+      swap_lanes<16>(x, y);
+      x += y;
+      y = x;
+    }
+    swap_lanes<32>(x, y);
+    o[e] = x + y;
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (sub == 0) reinterpret_cast<u32x2*>(out)[piece] = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+}
+
+// Few sequences, each in many pieces: four waves share the pieces of one query head, and a workgroup takes kJoinChannels of its channels.
+// (131071 keys of 28/4 heads: 14.8 us with all channels to a workgroup and one loop of dependent loads, 4.9 this way.)
+constexpr int kJoinChannels = 32;
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDecodeArgs a) {
+  constexpr int kLanes = kJoinChannels / 4, kSlots = kThreads / kLanes;       // lanes of a slot's channels; slots at a time
+  __shared__ f32x4 rows[kSlots][kLanes];
+  __shared__ float weights[kPagedMostWorkgroups], tops[kWaves], sums[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hq = blockIdx.x, seq = blockIdx.y;
+  const int head = (int)quotient((unsigned)hq, a.by_group), column = hq - head * a.group;
+  const Pieces p = pieces_of(a, seq, head, lane);
+  u16* const out = a.out + ((size_t)seq * a.n_q_heads + hq) * D + kJoinChannels * blockIdx.z;
+  if (p.n == 0 && tid < kLanes) reinterpret_cast<u32x2*>(out)[tid] = u32x2{0u, 0u};
+  if (p.n <= 1) return;
+  const unsigned n = p.n;
+  const float* const stats = a.partial + (size_t)2 * a.workgroups * a.group * D;
+  auto slot_of = [&](unsigned i) __attribute__((always_inline)) { return (size_t)piece_slot(p.first, p.w0 + i, p.share) * a.group + column; };
+  float top = -INFINITY;
+  for (unsigned i = tid; i < n; i += kThreads) {
+    weights[i] = stats[2 * slot_of(i)];
+    top = fmaxf(top, weights[i]);
+  }
+  top = over_wave(top, FloatMax{});
+  if (lane == 0) tops[wave] = top;
   __syncthreads();
-  if (sub != 0) return;
-  float top = -INFINITY, total = 0.f;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  top = tops[0];
 #pragma unroll
-  for (int i = 0; i < kSlots; ++i) top = fmaxf(top, tops[i]);
-#pragma unroll
-  for (int i = 0; i < kSlots; ++i) {
-    const float f = __builtin_amdgcn_exp2f(tops[i] - (top == -INFINITY ? 0.f : top));
-    total += f * sums[i];
-    sum += f * rows[i][piece];
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+  const float use = top == -INFINITY ? 0.f : top;
+  float total = 0.f;
+  for (unsigned i = tid; i < n; i += kThreads) {
+    const float f = __builtin_amdgcn_exp2f(weights[i] - use);
+    total += f * stats[2 * slot_of(i) + 1];
+    weights[i] = f;
   }
+  total = over_wave(total, FloatSum{});
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  const int sub = tid / kLanes, piece = tid % kLanes;
+  const float* const at = a.partial + kJoinChannels * blockIdx.z + 4 * piece;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (unsigned i = sub; i < n; i += kSlots) o += weights[i] * *reinterpret_cast<const f32x4*>(at + slot_of(i) * D);
+  rows[sub][piece] = o;
+  __syncthreads();
+  if (tid >= kLanes) return;
+  total = sums[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) total += sums[w];
+  const int in_use = min((int)n, kSlots);
+  f32x4 sum = rows[0][tid];
+  for (int i = 1; i < in_use; ++i) sum += rows[i][tid];
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  const u32x2 y = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
-  *reinterpret_cast<u32x2*>(a.out + ((size_t)seq * a.n_q_heads + hq) * D + 4 * piece) = y;
+  reinterpret_cast<u32x2*>(out)[tid] = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 
 template <int D, bool kE4m3>
 hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3>), dim3(a.workgroups), dim3(kThreads), (Shape<D, kE4m3>::kLds), s, a);
+  constexpr int kLds = Shape<D, kE4m3>::kLds;
+  if (a.direct) {
+    hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, true>), dim3(a.n_seqs * a.pool.n_heads), dim3(kThreads), kLds, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, false>), dim3(a.workgroups), dim3(kThreads), kLds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(paged_join_kernel<D>, dim3(a.n_q_heads, a.n_seqs), dim3(kThreads), 0, s, a);
+  // the sequences' query heads fit the chip four waves each, or else a wave each
+  if ((long long)a.n_q_heads * a.n_seqs * (D / kJoinChannels) <= 512)
+    hipLaunchKernelGGL(paged_join_many_kernel<D>, dim3(a.n_q_heads, a.n_seqs, D / kJoinChannels), dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL(paged_join_kernel<D>, dim3((a.n_q_heads + kWaves - 1) / kWaves, a.n_seqs), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 constexpr int kCus = 256;
+static_assert(kCus * 4 <= kPagedMostWorkgroups, "room for the weights of pieces");
 
 }  // namespace
 

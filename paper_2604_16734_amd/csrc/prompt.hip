@@ -53,12 +53,7 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
     const int s = min(base + lane, a.n_seqs - 1);
     const int begin = min(max(a.seq_begin[s], 0), a.n_tokens), end = min(max(a.seq_begin[s + 1], begin), a.n_tokens);
     const int tiles = base + lane < a.n_seqs ? (end - begin + kPromptRows - 1) / kPromptRows : 0;
-    int upto = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(upto, d);
-      upto += lane >= d ? y : 0;
-    }
+    const int upto = sum_upto(tiles);
     const unsigned long long there = __ballot(before + upto > rank);
     if (there != 0) {
       const int i = __builtin_ctzll(there);

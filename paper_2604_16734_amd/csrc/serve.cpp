@@ -76,6 +76,9 @@ float scale_log2_of(float scale, int head_dim) { return (scale > 0.f ? scale : 1
 
 }  // namespace
 
+// Sequences that can have no more tiles than this (by the width of the table) are not cut into pieces.
+constexpr unsigned long long kPagedDirectTiles = 8;
+
 // What a decode step needs: two places for partial results per workgroup, each of a KV head's query heads.
 static size_t paged_decode_bytes(const kvp_pages& p, int group) {
   return (size_t)2 * paged_decode_workgroups(p.head_dim, p.format == KVP_PAGE_E4M3) * group * (p.head_dim + 2) * sizeof(float);
@@ -109,6 +112,9 @@ int kvp_paged_decode(const kvp_pages* pages, const void* q, int64_t q_token, int
   a.width = table_width; a.n_seqs = n_seqs; a.n_q_heads = n_q_heads;
   a.group = n_q_heads / pages->n_kv_heads;
   a.workgroups = paged_decode_workgroups(pages->head_dim, e4m3);
+  a.direct = tiles <= kPagedDirectTiles ? 1 : 0;
+  a.by_heads = divisor_of((unsigned)pages->n_kv_heads, (unsigned)n_seqs * (unsigned)pages->n_kv_heads);
+  a.by_group = divisor_of((unsigned)a.group, (unsigned)n_q_heads);
   a.scale_log2 = scale_log2_of(softmax_scale, pages->head_dim);
   return code_of(launch_paged_decode(a, pages->head_dim, e4m3, static_cast<hipStream_t>(stream)));
 }

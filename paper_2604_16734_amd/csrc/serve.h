@@ -36,8 +36,12 @@ struct PagedDecodeArgs {
   long long q_token, q_head;
   int width, n_seqs, n_q_heads, group;
   int workgroups;
+  int direct;                 // one workgroup per sequence and KV head, nothing to join
+  Divisor by_heads;           // n_heads of the pool
+  Divisor by_group;
   float scale_log2;
 };
+constexpr int kPagedMostWorkgroups = 1024;
 int paged_decode_workgroups(int head_dim, bool e4m3);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);
 

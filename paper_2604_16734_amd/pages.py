@@ -1,14 +1,19 @@
 """Keys and values of many sequences in pages: a holder of the tensors, and the calls of include/kvp.h that serve many sequences at
-once with torch tensors as their arguments.  Marshalling only, as in binding.py."""
+once with torch tensors as their arguments.  Marshalling only, as in binding.py; calls on torch's current stream and device go
+through csrc/fast_calls.cpp, and what it does not take through Python, which says what is wrong."""
 import contextlib
 import ctypes
 
+from .binding import _entries, _fast_call
 from .binding import KVP_EINVAL, KVP_PAGE_BF16, KVP_PAGE_E4M3, KvpError, KvpPages, KvpPrompts, KvpRows, lib
 
 
 def _need(ok, what):
     if not ok:
         raise KvpError(KVP_EINVAL, what)
+
+
+_prompt = None
 
 
 class _On:
@@ -63,7 +68,16 @@ def prompt_attention(q, k, v, seq_begin, out=None, softmax_scale=0.0, stream=Non
     of k and v [n_tokens, n_kv_heads, d], any strides but the last (kvp_prompt_attention).  Rows behind the last prompt are left as they
     were in `out`; without one given they hold whatever was there."""
     import torch
+    global _prompt
     what, device = "prompt_attention: ", q.device
+    if stream is None and out is not None and device.index is not None and torch._C._cuda_getDevice() == device.index:
+        if _prompt is None:
+            _prompt = _fast_call("prompt")
+        rc = _prompt(_entries.kvp_prompt_attention, device.index, torch._C._cuda_getCurrentRawStream(device.index), q, k, v, seq_begin, out, softmax_scale)
+        if rc == 0:
+            return out
+        if rc is not None:
+            raise KvpError(rc, "kvp_prompt_attention")
     _need(q.dim() == 3 and k.dim() == 3 and device.type == "cuda" and device.index is not None, what + "q and k")
     (n_tokens, n_q_heads, d), n_kv_heads, n_seqs = q.shape, k.shape[1], seq_begin.numel() - 1
     at = [_numbers(q, (n_tokens, n_q_heads, d), device, what + "q")]
@@ -100,6 +114,10 @@ class Pages:
         self.of = KvpPages(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if e4m3 else None, v_exp.data_ptr() if e4m3 else None,
                            KVP_PAGE_E4M3 if e4m3 else KVP_PAGE_BF16, *k.shape)
         self._ref, self._lib = ctypes.byref(self.of), lib()
+        # what every call needs, looked up once (a step of a few sequences takes the GPU 4 us; through Python alone a call took the host 8)
+        self._at, self._index = ctypes.addressof(self.of), k.device.index
+        self._native_rows, self._native_decode = _fast_call("page_rows"), _fast_call("paged_decode")
+        self._device, self._stream, self._work = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, {}
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, page_size=64, e4m3=False, device="cuda:0"):
@@ -112,6 +130,13 @@ class Pages:
         return cls(new(shape, torch.float8_e4m3fn), new(shape, torch.float8_e4m3fn), new(shape[:3], torch.uint8), new(shape[:3], torch.uint8))
 
     def _rows(self, call, k, v, seq_begin, table, first, stream):
+        if stream is None and self._device() == self._index:
+            rc = self._native_rows(getattr(_entries, "kvp_page_" + call), self._at, self.n_kv_heads, self.head_dim, self._index, self._stream(self._index),
+                                   k, v, seq_begin, table, first)
+            if rc == 0:
+                return
+            if rc is not None:
+                raise KvpError(rc, "kvp_page_" + call)
         n_tokens, n_seqs, device = k.shape[0], seq_begin.numel() - 1, self.device
         what = "Pages.%s: " % call
         shape = (n_tokens, self.n_kv_heads, self.head_dim)
@@ -136,12 +161,17 @@ class Pages:
         """The way back, into k and v (kvp_page_read)."""
         self._rows("read", k, v, seq_begin, table, first, stream)
 
+    def _workspace_bytes(self, n_q_heads):
+        nbytes = self._work.get(n_q_heads)
+        if nbytes is None:
+            nbytes = self._work[n_q_heads] = self._lib.kvp_paged_decode_bytes(self._ref, n_q_heads)
+        _need(nbytes > 0, "Pages.decode: n_q_heads")
+        return nbytes
+
     def workspace(self, n_q_heads):
         """Room for the partial results of a decode step with this many query heads; steps that may overlap need one each."""
         import torch
-        nbytes = self._lib.kvp_paged_decode_bytes(self._ref, n_q_heads)
-        _need(nbytes > 0, "Pages.workspace: n_q_heads")
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return torch.empty(self._workspace_bytes(n_q_heads), dtype=torch.uint8, device=self.device)
 
     def decode(self, q, table, lengths, out=None, softmax_scale=0.0, workspace=None, stream=None):
         """One token of every sequence: q [n_seqs, n_q_heads, head_dim] over tokens 0 .. lengths[s] - 1 of the pages table[s]
@@ -150,6 +180,15 @@ class Pages:
         n_seqs, device = lengths.numel(), self.device
         _need(q.dim() == 3 and table.dim() == 2, "Pages.decode: q and table")
         n_q_heads, what = q.shape[1], "Pages.decode: "
+        if stream is None and self._device() == self._index:
+            if out is None:
+                out = torch.empty((n_seqs, n_q_heads, self.head_dim), dtype=torch.bfloat16, device=device)
+            rc = self._native_decode(_entries.kvp_paged_decode, self._at, n_q_heads, self.head_dim, self._index, self._stream(self._index), q, table, lengths,
+                                     out, self._workspace_bytes(n_q_heads) if workspace is None else workspace, softmax_scale)
+            if rc == 0:
+                return out
+            if rc is not None:
+                raise KvpError(rc, "kvp_paged_decode")
         shape = (n_seqs, n_q_heads, self.head_dim)
         q_at, q_token, q_head = _numbers(q, shape, device, what + "q")
         table_at = _whole(table, (n_seqs, table.shape[1]), device, what + "table")
