@@ -43,7 +43,9 @@ struct Shape {
   static_assert(kLds <= 64 * 1024, "LDS that a kernel has without asking");
 };
 
-// Tile of 128 rows number `rank` of a list that goes through the sequences: each sequence's tiles, the last one, which sees most keys, first.
+// Tile of 128 rows number `rank` of a list of all sequences' tiles, those that see most keys first, so that the workgroups that come last are the
+// short ones: tile t of a sequence comes before all tiles t - 1.  With more than 64 sequences the list goes through the sequences instead, each
+// one's last tile first: a look at all of them for every step of the search would take longer than it saves.
 struct PromptTile {
   int begin, length, tile;            // the sequence's first row and its rows; length 0: no such tile
 };
@@ -54,6 +56,21 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
     const int begin = min(max(a.seq_begin[s], 0), a.n_tokens), end = min(max(a.seq_begin[s + 1], begin), a.n_tokens);
     const int tiles = base + lane < a.n_seqs ? (end - begin + kPromptRows - 1) / kPromptRows : 0;
     const int upto = sum_upto(tiles);
+    if (a.n_seqs <= 64) {
+      if (__builtin_amdgcn_readlane(upto, 63) <= rank) break;
+      // the t with  tiles from t + 1 on <= rank < tiles from t on
+      int lo = 0, hi = a.n_tokens / kPromptRows + 1, from_hi = 0;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2, n = sum_of_wave(max(tiles - mid, 0));
+        if (n > rank) lo = mid;
+        else hi = mid, from_hi = n;
+      }
+      // of the sequences that have a tile lo, the one before which so many come
+      unsigned long long there = __ballot(tiles > lo);
+      for (int skip = rank - from_hi; skip > 0; --skip) there &= there - 1;
+      const int i = __builtin_ctzll(there);
+      return PromptTile{__builtin_amdgcn_readlane(begin, i), __builtin_amdgcn_readlane(end - begin, i), lo};
+    }
     const unsigned long long there = __ballot(before + upto > rank);
     if (there != 0) {
       const int i = __builtin_ctzll(there);
@@ -66,7 +83,7 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const PromptArgs a) {
+__global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(const PromptArgs a) {
   using S = Shape<D>;
   constexpr int kNK = D / 16, kNV = (D / 32) * 2, kND = D / 32;       // K and V fragments of a block of 32 keys; channel tiles
   extern __shared__ __align__(16) unsigned char lds_raw[];
@@ -75,16 +92,11 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const PromptArgs a)
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // a die has heads of its own where they can be dealt out evenly: its L2 then holds the K and V of these alone
-  const int xcd = blockIdx.x % kXcds, item = blockIdx.x / kXcds;
-  int h, rank;
-  if (a.heads_per_xcd > 0) {
-    rank = (int)quotient((unsigned)item, a.by_heads);
-    h = xcd * a.heads_per_xcd + item - rank * a.heads_per_xcd;
-  } else {
-    rank = (int)quotient(blockIdx.x, a.by_heads);
-    h = (int)blockIdx.x - rank * a.n_q_heads;
-  }
+  // Dies and KV heads are dealt out to each other: dies_per_set dies share the query heads of as few KV heads as that allows, whose K and V
+  // their L2 caches then hold, and take turns along the list of (tile, query head).
+  const int xcd = blockIdx.x % kXcds, set = xcd / a.dies_per_set;
+  const unsigned item = blockIdx.x / kXcds * (unsigned)a.dies_per_set + (unsigned)(xcd - set * a.dies_per_set);
+  const int rank = (int)quotient(item, a.by_set_heads), h = set * a.set_heads + (int)item - rank * a.set_heads;
   const PromptTile pt = find_tile(a, rank, lane);
   const int n = pt.length, wg_row = pt.tile * kPromptRows;
   if (wg_row >= n) return;
@@ -117,19 +129,25 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const PromptArgs a)
   }
   struct Feed {
     unsigned long long at;
-    unsigned tile_bytes, row_bytes;
+    unsigned bytes, row_bytes;
     int rows;                          // from this tile's first one on
+  };
+  auto bytes_of = [&](int rows, unsigned row_bytes) __attribute__((always_inline)) -> unsigned {      // up to the end of the last row (no branches)
+    return (unsigned)max(min(max(rows, 0), kTileKeys) * (int)row_bytes - (int)(row_bytes - 2u * D), 0);
+  };
+  auto feed_at = [&](const u16* first, unsigned row_bytes, int rows) __attribute__((always_inline)) -> Feed {
+    return Feed{(unsigned long long)first, bytes_of(rows, row_bytes), row_bytes, rows};
   };
   auto load_fed = [&](const Feed& f, const unsigned (&of)[S::kLoads], auto which, unsigned to) __attribute__((always_inline)) {
     constexpr int j = decltype(which)::value;
-    const unsigned bytes = f.rows >= kTileKeys ? f.tile_bytes : f.rows > 0 ? (unsigned)(f.rows - 1) * f.row_bytes + 2u * D : 0u;
-    const u32x4 buffer = {(unsigned)f.at, (unsigned)(f.at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+    const u32x4 buffer = {(unsigned)f.at, (unsigned)(f.at >> 32) & 0xFFFFu, f.bytes, 0x00020000u};
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen offset:%3 lds" ::"v"(of[j]), "s"(buffer), "s"(to), "n"(1024 * j)
                  : "m0", "memory");
   };
   auto move_on = [&](Feed& f) __attribute__((always_inline)) {
-    f.at += f.tile_bytes;
+    f.at += (unsigned long long)kTileKeys * f.row_bytes;
     f.rows -= kTileKeys;
+    f.bytes = bytes_of(f.rows, f.row_bytes);
   };
   auto load_tile = [&](const Feed& f, const unsigned (&of)[S::kLoads], unsigned to) __attribute__((always_inline)) {
     load_fed(f, of, std::integral_constant<int, 0>{}, to);
@@ -170,8 +188,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const PromptArgs a)
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of), "s"(buffer), "s"(to + 1024u * j) : "m0", "memory");
     }
   }
-  Feed k_feed{(unsigned long long)k_rows, kTileKeys * a.k_bytes, a.k_bytes, rows_end};
-  Feed v_feed{(unsigned long long)v_rows, kTileKeys * a.v_bytes, a.v_bytes, rows_end};
+  Feed k_feed = feed_at(k_rows, a.k_bytes, rows_end), v_feed = feed_at(v_rows, a.v_bytes, rows_end);
   load_tile(k_feed, k_lane, lds_dst(lds_k));
   load_tile(v_feed, v_lane, lds_dst(lds_v));
   move_on(k_feed);

@@ -55,10 +55,9 @@ struct PromptArgs {
   long long q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
   unsigned q_bytes, k_bytes, v_bytes;      // from token to token
   int n_tokens, n_seqs, n_q_heads;
-  int heads_per_xcd;          // 0: the heads cannot be dealt out evenly
+  int dies_per_set, set_heads;             // dies that share set_heads query heads
   unsigned workgroups;
-  Divisor by_heads;           // heads_per_xcd, or n_q_heads
-  Divisor by_group;
+  Divisor by_set_heads, by_group;
   float scale_log2;
 };
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s);
