@@ -27,27 +27,30 @@
 namespace kvp {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = kPagedTile / kWaves;      // keys of a wave's part of a tile
+constexpr int kKeys = 32;                      // keys of a wave's part of a tile: two blocks of 16
 constexpr int kHeads = 16;                     // columns of the products
-static_assert(kKeys == 32, "two blocks of 16 keys");
+constexpr int kAloneWaves = 8;
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
-template <int D, bool kE4m3>
+// Ways to spread the work: in shares, as above; or a workgroup for every sequence and KV head, with nothing to join.
+enum Way { kShares, kAlone };
+
+template <int D, bool kE4m3, Way kWay>
 struct Shape {
+  static constexpr int kWaves = kWay == kShares ? kPagedTile / kKeys : kAloneWaves;
+  static constexpr int kThreads = 64 * kWaves, kTile = kKeys * kWaves;
   static constexpr int kRow = kE4m3 ? D : 2 * D;                  // bytes of a row in the pages
   static constexpr int kChunks = kRow / 16;
   static constexpr int kLoads = kRow / 64;                        // of 1 KiB, for 16 rows
   static constexpr int kStrip = kKeys * kRow;
   static constexpr int kExps = kE4m3 ? 256 : 0;
-  static constexpr int kWaveBytes = 2 * kStrip + kExps;
+  static constexpr int kWaveBytes = 2 * kStrip + kExps;           // K, V, exponents
   static constexpr int kLds = kWaves * kWaveBytes;
-  static constexpr int kPerCu = kLds > 40 * 1024 ? 2 : 4;         // workgroups of a CU
+  static constexpr int kPerCu = kLds > 80 * 1024 ? 1 : kLds > 40 * 1024 || kWaves == 8 ? 2 : 4;      // workgroups of a CU
   // what a wave leaves of a piece lies over its strips: the output as it is in the accumulators, then maxima and sums
-  static constexpr int kOut = kHeads * D * 4;
-  static constexpr int kStat = kE4m3 ? 2 * kStrip : kOut;
+  static constexpr int kOut = kHeads * D * 4, kStat = kE4m3 ? 2 * kStrip : kOut;
   static_assert(kOut <= 2 * kStrip && kStat + 2 * kHeads * 4 <= kWaveBytes, "room for a piece");
-  static_assert(kLds <= 64 * 1024, "LDS that a kernel has without asking");
 };
 
 // In LDS the 16-byte chunk ch of row r lies at position ch ^ f(r), for reads free of bank conflicts.  K is read in chunks of one
@@ -61,14 +64,16 @@ __device__ __forceinline__ int v_swizzle_of(int row) {
   else return row / (256 / kRow) % (kRow / 32) + kRow / 32 * (row / 16 % 2);
 }
 
-// eight e4m3 numbers as bf16, exactly
-__device__ __forceinline__ bf16x8 eight_of_e4m3(unsigned lo, unsigned hi) {
-  const u32x4 w = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false)),
-                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true)),
-                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false)),
-                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true))};
+// eight e4m3 numbers times a power of two as bf16, exactly
+__device__ __forceinline__ bf16x8 eight_of_e4m3(unsigned lo, unsigned hi, float by) {
+  const u32x4 w = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false)),
+                   __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true))};
   return __builtin_bit_cast(bf16x8, w);
 }
+// the larger one, in one instruction (fmaxf makes NaNs quiet first, with one more for each operand)
+__device__ __forceinline__ float max_of(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
 // 2^e of the i-th of four exponents
 __device__ __forceinline__ float power_of(unsigned exps, int i) {
   return __uint_as_float((i < 3 ? exps << (23 - 8 * i) : exps >> 1) & 0x7F800000u);
@@ -84,11 +89,13 @@ __device__ __forceinline__ bf16x8 lds_read_vt16(const unsigned char* p, int rows
 __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, int seq) {
   return seq < a.n_seqs ? min(max(a.lengths[seq], 0), a.width << a.pool.shift) : 0;
 }
-// kDirect: workgroup b has all of sequence b / n_heads, KV head b % n_heads, and there is nothing to join.
-template <int D, bool kE4m3, bool kDirect>
-__global__ void __launch_bounds__(kThreads, (Shape<D, kE4m3>::kPerCu * kWaves / 4))
+// Not in shares: workgroup b has all of sequence b / n_heads, KV head b % n_heads, and there is nothing to join.
+template <int D, bool kE4m3, Way kWay>
+__global__ void __launch_bounds__((Shape<D, kE4m3, kWay>::kThreads), (Shape<D, kE4m3, kWay>::kPerCu * Shape<D, kE4m3, kWay>::kWaves / 4))
 paged_decode_kernel(const PagedDecodeArgs a) {
-  using S = Shape<D, kE4m3>;
+  using S = Shape<D, kE4m3, kWay>;
+  constexpr bool kDirect = kWay == kAlone;
+  constexpr int kWaves = S::kWaves, kThreads = S::kThreads, kTile = S::kTile;
   constexpr int kRow = S::kRow, kChunks = S::kChunks, kLoads = S::kLoads;
   constexpr int kSteps = D / 32;                 // products with K of a block of 16 keys
   constexpr int kTiles = D / 16;                 // channel tiles of the output
@@ -113,14 +120,12 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     seq = (int)quotient(blockIdx.x, a.by_heads);
     direct_head = (int)blockIdx.x - seq * a.pool.n_heads;
     ids = lane < a.width ? a.table[(size_t)seq * a.width + lane] : -1;       // (beside the length, not after it)
-    n_keys = length_of(a, seq);
+    n_keys = __builtin_amdgcn_readfirstlane(length_of(a, seq));
     if (n_keys == 0) {
       for (int i = threadIdx.x; i < a.group * D / 8; i += kThreads)
         reinterpret_cast<u32x4*>(a.out + ((size_t)seq * a.n_q_heads + direct_head * a.group) * D)[i] = u32x4{0u, 0u, 0u, 0u};
       return;
     }
-    ids = ids < a.pool.n_pages ? ids : -1;
-    asm volatile("" : "+v"(ids));
   } else {
     next_group(0);
     int others = 0;
@@ -143,46 +148,43 @@ paged_decode_kernel(const PagedDecodeArgs a) {
   // ---- global -> LDS.  Load i of 16 rows brings in rows 1024 / kRow * i + ..; its immediate offset moves both of its addresses by 1 KiB.
   // (Inline assembly, and waits of this kernel's own: the compiler would have every read of LDS wait for all loads.  s_nop: a load may read a
   // scalar register five wait states after a vector instruction has written it.)
-  unsigned k_lane[kLoads], v_lane[kLoads];
+  unsigned k_lane[kLoads], v_lane[2][kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int sub = lane / kChunks, pos = lane % kChunks, row = 1024 / kRow * i + sub;
     k_lane[i] = (unsigned)(sub * kRow + 16 * (pos ^ k_swizzle<kRow>(row)));
-    v_lane[i] = (unsigned)(sub * kRow + 16 * (pos ^ v_swizzle_of<kRow, kE4m3>(row)));
+#pragma unroll
+    for (int b = 0; b < 2; ++b) v_lane[b][i] = (unsigned)(sub * kRow + 16 * (pos ^ v_swizzle_of<kRow, kE4m3>(16 * b + row)));
   }
-  auto load_rows = [&](u32x4 buffer, const unsigned (&of)[kLoads], unsigned flip, unsigned to) __attribute__((always_inline)) {
+  auto load_rows = [&](u32x4 buffer, const unsigned (&of)[kLoads], unsigned to) __attribute__((always_inline)) {
     if constexpr (kLoads == 4)
       asm volatile("s_mov_b32 m0, %5\n\ts_nop 3\n\t"
                    "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
                    "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
                    "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
-                   "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds" ::"v"(of[0] ^ flip), "v"(of[1] ^ flip), "v"(of[2] ^ flip),
-                   "v"(of[3] ^ flip), "s"(buffer), "s"(to)
+                   "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds" ::"v"(of[0]), "v"(of[1]), "v"(of[2]), "v"(of[3]), "s"(buffer), "s"(to)
                    : "m0", "memory");
     else if constexpr (kLoads == 2)
       asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\t"
                    "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
-                   "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds" ::"v"(of[0] ^ flip), "v"(of[1] ^ flip), "s"(buffer), "s"(to)
+                   "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds" ::"v"(of[0]), "v"(of[1]), "s"(buffer), "s"(to)
                    : "m0", "memory");
     else
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\t"
-                   "buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of[0] ^ flip), "s"(buffer), "s"(to)
+                   "buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of[0]), "s"(buffer), "s"(to)
                    : "m0", "memory");
   };
   auto buffer_at = [&](const char* base, int rows) __attribute__((always_inline)) -> u32x4 {
     const unsigned long long x = (unsigned long long)base;
-    // (through the first lane: for the compiler a quotient is no scalar, and neither is what follows from it)
-    return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)x), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32) & 0xFFFFu),
-                 (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(rows * kRow)), 0x00020000u};
+    // (through the first lane: the compiler would carry some of it in vector registers)
+    return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((int)x), (unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) & 0xFFFFu,
+                 (unsigned)__builtin_amdgcn_readfirstlane(rows * kRow), 0x00020000u};
   };
   auto wait_all_but = [&](auto newest) __attribute__((always_inline)) {
     constexpr int k = decltype(newest)::value;
-    static_assert(k < 16);
-    __builtin_amdgcn_s_waitcnt(0x0F70 | k);
+    static_assert(k < 64);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (k & 15) | (k >> 4 << 14));
     asm volatile("" ::: "memory");
-  };
-  auto strips_read = [&]() __attribute__((always_inline)) {          // what was read from LDS is in registers
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
   typedef std::integral_constant<int, 2 * kLoads + (kE4m3 ? 1 : 0)> KLoads;      // of a tile: exponents and K
   typedef std::integral_constant<int, 2 * kLoads> VLoads;
@@ -217,22 +219,27 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       seq_end = before + (unsigned)__builtin_amdgcn_readlane((int)upto, i);
       seq_first = seq_end - (unsigned)__builtin_amdgcn_readlane((int)tiles, i);
     }
-    const unsigned n_tiles = (unsigned)paged_tiles(n_keys);
+    const unsigned n_tiles = (unsigned)(n_keys + kTile - 1) / kTile;
     const int head = kDirect ? direct_head : __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
     const unsigned first = seq_first + (unsigned)head * n_tiles;      // the first unit of this sequence and head
     const int t0 = kDirect ? 0 : (int)(at - first), t1 = kDirect ? (int)n_tiles : (int)(min(end, first + n_tiles) - first);
     const int32_t* const row_of_table = a.table + (size_t)seq * a.width;
 
-    // the page numbers of 64 columns from col0 on; -1: no such page
+    // where the rows of 64 columns from col0 on begin, for this head, in rows of the pages; negative: no such page
     int col0 = 0;
+    long long page_rows = -1;
+    auto rows_of_ids = [&]() __attribute__((always_inline)) {
+      page_rows = ids < 0 || ids >= a.pool.n_pages ? -1ll : (long long)page_row(ids, a.pool.n_heads, head, 0, a.pool.shift);
+      asm volatile("" : "+v"(page_rows));               // here, not where it is used: the wait there would be for all loads, every time
+    };
     auto load_ids = [&](int col) __attribute__((always_inline)) {
       col0 = col;
-      const int id = col + lane < a.width ? row_of_table[col + lane] : -1;
-      ids = id < a.pool.n_pages ? id : -1;
-      asm volatile("" : "+v"(ids));               // here, not where it is used: the wait there would be for all loads, every time
+      ids = col + lane < a.width ? row_of_table[col + lane] : -1;
+      rows_of_ids();
     };
-    const int kb0 = kPagedTile * t0 + kKeys * wave;
-    if (!kDirect && kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
+    const int kb0 = kTile * t0 + kKeys * wave;
+    if (kDirect) rows_of_ids();
+    else if (kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
 
     // Q: second operand, column l16 of the products; channels in the order of K's fragments
     bf16x8 qf[kSteps];
@@ -252,60 +259,53 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     // rows of the two blocks of a tile that take part, and where they are
     struct Tile {
       int rows[2];
-      unsigned long long at[2];                   // row numbers in the pages
+      long long at[2];
     };
+    const int my_end = min(t1, (n_keys - kKeys * wave + kTile - 1) / kTile);      // tiles in which this wave has keys
     auto tile_at = [&](int t) __attribute__((always_inline)) -> Tile {
-      const int kb = kPagedTile * t + kKeys * wave;
+      const int kb = kTile * t + kKeys * wave;
       Tile x;
       if (((kb + 16) >> a.pool.shift) - col0 >= 64) load_ids(kb >> a.pool.shift);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const PagePlace p = place_of(kb + 16 * b, a.pool.shift);
-        const int id = __builtin_amdgcn_readlane(ids, p.column - col0);
-        x.rows[b] = id < 0 ? 0 : min(16, max(0, n_keys - kb - 16 * b));
-        x.at[b] = page_row(max(id, 0), a.pool.n_heads, head, p.offset, a.pool.shift);
+        const int hi = __builtin_amdgcn_readlane((int)(page_rows >> 32), p.column - col0), none = hi >> 31;       // (no branches)
+        const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)page_rows, p.column - col0);
+        x.rows[b] = min(16, max(0, n_keys - kb - 16 * b)) & ~none;
+        x.at[b] = (long long)((unsigned long long)(unsigned)(hi & ~none) << 32 | (lo & ~(unsigned)none)) + p.offset;
       }
       return x;
     };
     auto issue_k = [&](const Tile& x) __attribute__((always_inline)) {
+      const unsigned to = lds_at;
       if constexpr (kE4m3) {                      // four exponents a lane: of block lane / 4 % 2, K's and V's
-        const unsigned long long row = lane & 4 ? x.at[1] : x.at[0];
+        const long long row = lane & 4 ? x.at[1] : x.at[0];
         const uint8_t* const src = (lane & 8 ? a.pool.v_exp : a.pool.k_exp) + row + 4 * (lane & 3);
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_at + 2 * S::kStrip) : "m0", "memory");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(to + 2 * S::kStrip) : "m0", "memory");
       }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.k + x.at[b] * kRow, x.rows[b]), k_lane, 0, lds_at + b * 16 * kRow);
+      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.k + x.at[b] * kRow, x.rows[b]), k_lane, to + b * 16 * kRow);
     };
     auto issue_v = [&](const Tile& x) __attribute__((always_inline)) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-        load_rows(buffer_at(a.pool.v + x.at[b] * kRow, x.rows[b]), v_lane, b ? 16u * (unsigned)v_swizzle_of<kRow, kE4m3>(16) : 0u,
-                  lds_at + S::kStrip + b * 16 * kRow);
+      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.v + x.at[b] * kRow, x.rows[b]), v_lane[b], lds_at + S::kStrip + b * 16 * kRow);
     };
 
-    const int my_end = min(t1, (n_keys - kKeys * wave + kPagedTile - 1) / kPagedTile);      // tiles in which this wave has keys
-    Tile next{};
+    Tile next{{0, 0}, {0, 0}};
     if (t0 < my_end) {
       next = tile_at(t0);
       issue_k(next);
       issue_v(next);
-    }
 #pragma unroll
-    for (int st = 0; st < kSteps; ++st) asm volatile("" : "+v"(qf[st]));         // likewise
+      for (int st = 0; st < kSteps; ++st) asm volatile("" : "+v"(qf[st]));         // (as page_rows)
+    }
     for (int t = t0; t < my_end; ++t) {
       const Tile now = next;
       const bool more = t + 1 < my_end;
       // ---- logits
       wait_all_but(VLoads{});
-      unsigned k_exp[2], v_exp[2];
-      if constexpr (kE4m3) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          k_exp[b] = *reinterpret_cast<const unsigned*>(exps + 4 * (4 * b + g));
-          v_exp[b] = *reinterpret_cast<const unsigned*>(exps + 4 * (8 + 4 * b + g));
-        }
-      }
       f32x4 s[2];
+      unsigned v_exp[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -316,12 +316,14 @@ paged_decode_kernel(const PagedDecodeArgs a) {
             s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], s[b], 0, 0, 0);
           }
         } else {
+          v_exp[b] = *reinterpret_cast<const unsigned*>(exps + 32 + 16 * b + 4 * g);
+          const float by = __uint_as_float((unsigned)exps[16 * b + l16] << 23);       // of the key whose numbers this lane has
 #pragma unroll
           for (int st = 0; st < kSteps; st += 2) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(k_strip + b * 16 * kRow + k_off[st]);
 #pragma unroll
             for (int half = 0; half < 2; ++half)
-              s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_of_e4m3(w[2 * half], w[2 * half + 1]), qf[st + half], s[b], 0, 0, 0);
+              s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_of_e4m3(w[2 * half], w[2 * half + 1], by), qf[st + half], s[b], 0, 0, 0);
           }
         }
       }
@@ -334,22 +336,18 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       }
       // ---- weights
       const bool masked = now.rows[0] + now.rows[1] < kKeys;
-      float top = -INFINITY;
+      if (masked) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if constexpr (kE4m3) s[b][r] *= power_of(k_exp[b], r);
-          if (masked) s[b][r] = 4 * g + r < now.rows[b] ? s[b][r] : -INFINITY;
-          top = fmaxf(top, s[b][r]);
-        }
+        for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 4 * g + i % 4 < now.rows[i / 4] ? s[i / 4][i % 4] : -INFINITY;
+      }
+      float top = max_of(max_of(max_of(s[0][0], s[0][1]), max_of(s[0][2], s[0][3])), max_of(max_of(s[1][0], s[1][1]), max_of(s[1][2], s[1][3])));
       {
         float y = top;
         swap_lanes<16>(top, y);
-        top = fmaxf(top, y);
+        top = max_of(top, y);
         y = top;
         swap_lanes<32>(top, y);
-        top = fmaxf(top, y);
+        top = max_of(top, y);
       }
       if (__any(top > m)) {                       // a larger logit: what has been added up is brought onto it
         const float m_new = fmaxf(m, top);
@@ -365,10 +363,11 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       for (int i = 0; i < 8; ++i) {
         p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], sl2, minus));
         l += p[i];
-        if constexpr (kE4m3) {
-          p[i] *= power_of(v_exp[i / 4], i % 4);
-          if (masked) p[i] = 4 * g + i % 4 < now.rows[i / 4] ? p[i] : 0.f;      // (no row, no exponent)
-        }
+        if constexpr (kE4m3) p[i] *= power_of(v_exp[i / 4], i % 4);
+      }
+      if (kE4m3 && masked) {                      // no row, no exponent
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = 4 * g + i % 4 < now.rows[i / 4] ? p[i] : 0.f;
       }
       const u32x4 pw = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
       const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
@@ -381,15 +380,15 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         if constexpr (!kE4m3) vf = lds_read_vt16(v_strip + v_off[dt], 16 * kRow);
         else {
           const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(v_strip + v_off[dt]));
-          vf = eight_of_e4m3((unsigned)w[0], (unsigned)w[1]);
+          vf = eight_of_e4m3((unsigned)w[0], (unsigned)w[1], 1.f);
         }
         o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[dt], 0, 0, 0);
       }
-      strips_read();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) issue_v(next);
     }
 
-    // ---- the four waves' results of the piece, joined
+    // ---- the waves' results of the piece, joined
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[dt]));        // (as above)
     {
@@ -411,9 +410,9 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     const bool whole = kDirect || piece_is_whole(first, n_tiles, share);
     const size_t slot = kDirect ? 0 : (size_t)piece_slot(first, blockIdx.x, share) * a.group;
 #pragma unroll
-    for (int i = 0; i < 64 * kTiles / kThreads; ++i) {
+    for (int i = 0; i < (64 * kTiles + kThreads - 1) / kThreads; ++i) {
       const int item = kThreads * i + threadIdx.x, column = item % 16, ch = 16 * (item / 64) + 4 * (item / 16 % 4);
-      if (column >= a.group) continue;
+      if (column >= a.group || item >= 64 * kTiles) continue;
       float top = -INFINITY, f[kWaves], total = 0.f;
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -446,6 +445,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
 
 // ---- the pieces of one sequence and query head, joined; a sequence without keys has zeros.  First their weights, then the weighted sum, whose
 // loads do not wait for one another.
+constexpr int kJoinWaves = 4, kJoinThreads = 64 * kJoinWaves;
 struct Pieces {
   unsigned first, n_tiles, share, w0, n;       // first unit, units; the workgroups that have pieces are w0 .. w0 + n - 1; n = 1: whole
 };
@@ -468,9 +468,9 @@ __device__ __forceinline__ Pieces pieces_of(const PagedDecodeArgs& a, int seq, i
 
 // Many sequences: a wave for each query head of one.  (96 sequences, 32/8 heads, d 128: 15.8 us with the kernel below, 5.0 this way.)
 template <int D>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedDecodeArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDecodeArgs a) {
   constexpr int kLanes = D / 4, kSlots = 64 / kLanes;
-  const int lane = threadIdx.x & 63, seq = blockIdx.y, hq = kWaves * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, seq = blockIdx.y, hq = kJoinWaves * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (hq >= a.n_q_heads) return;
   const int head = (int)quotient((unsigned)hq, a.by_group), column = hq - head * a.group;
   const Pieces p = pieces_of(a, seq, head, lane);
@@ -518,10 +518,10 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedDecodeA
 constexpr int kJoinChannels = 32;
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDecodeArgs a) {
-  constexpr int kLanes = kJoinChannels / 4, kSlots = kThreads / kLanes;       // lanes of a slot's channels; slots at a time
+__global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const PagedDecodeArgs a) {
+  constexpr int kLanes = kJoinChannels / 4, kSlots = kJoinThreads / kLanes;       // lanes of a slot's channels; slots at a time
   __shared__ f32x4 rows[kSlots][kLanes];
-  __shared__ float weights[kPagedMostWorkgroups], tops[kWaves], sums[kWaves];
+  __shared__ float weights[kPagedMostWorkgroups], tops[kJoinWaves], sums[kJoinWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hq = blockIdx.x, seq = blockIdx.y;
   const int head = (int)quotient((unsigned)hq, a.by_group), column = hq - head * a.group;
   const Pieces p = pieces_of(a, seq, head, lane);
@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDe
   const float* const stats = a.partial + (size_t)2 * a.workgroups * a.group * D;
   auto slot_of = [&](unsigned i) __attribute__((always_inline)) { return (size_t)piece_slot(p.first, p.w0 + i, p.share) * a.group + column; };
   float top = -INFINITY;
-  for (unsigned i = tid; i < n; i += kThreads) {
+  for (unsigned i = tid; i < n; i += kJoinThreads) {
     weights[i] = stats[2 * slot_of(i)];
     top = fmaxf(top, weights[i]);
   }
@@ -541,10 +541,10 @@ __global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDe
   __syncthreads();
   top = tops[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+  for (int w = 1; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
   const float use = top == -INFINITY ? 0.f : top;
   float total = 0.f;
-  for (unsigned i = tid; i < n; i += kThreads) {
+  for (unsigned i = tid; i < n; i += kJoinThreads) {
     const float f = __builtin_amdgcn_exp2f(weights[i] - use);
     total += f * stats[2 * slot_of(i) + 1];
     weights[i] = f;
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDe
   if (tid >= kLanes) return;
   total = sums[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) total += sums[w];
+  for (int w = 1; w < kJoinWaves; ++w) total += sums[w];
   const int in_use = min((int)n, kSlots);
   f32x4 sum = rows[0][tid];
   for (int i = 1; i < in_use; ++i) sum += rows[i][tid];
@@ -570,33 +570,55 @@ __global__ void __launch_bounds__(kThreads) paged_join_many_kernel(const PagedDe
   reinterpret_cast<u32x2*>(out)[tid] = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 
+constexpr int kCus = 256;
+static_assert(kCus * 4 <= kPagedMostWorkgroups, "room for the weights of pieces");
+// A workgroup of its own for every sequence and KV head: where no sequence can have more keys than this, by the width of the table; more
+// where there are so many that all CUs have one.  8 KV heads, d 128, e4m3, alone and in shares: one sequence of 512 keys 5.8 and 8.1 us, 768 7.0
+// and 8.2, 1024 8.9 and 8.2; 32 sequences of 512 7.2 and 13.0, of 1000 13.4 and 18.5, of 2500 27.1 and 32.0, of 2500 once and 300 else 15.6 and 13.8.
+constexpr long long kAloneKeys = 768, kAloneKeysOfMany = 2560;
+
 template <int D, bool kE4m3>
 hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {
-  constexpr int kLds = Shape<D, kE4m3>::kLds;
-  if (a.direct) {
-    hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, true>), dim3(a.n_seqs * a.pool.n_heads), dim3(kThreads), kLds, s, a);
+  const unsigned pairs = (unsigned)a.n_seqs * (unsigned)a.pool.n_heads;
+  if (a.most_keys <= (pairs >= kCus ? kAloneKeysOfMany : kAloneKeys)) {
+    using S = Shape<D, kE4m3, kAlone>;
+    hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kAlone>), dim3(pairs), dim3(S::kThreads), S::kLds, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, false>), dim3(a.workgroups), dim3(kThreads), kLds, s, a);
+  using S = Shape<D, kE4m3, kShares>;
+  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kShares>), dim3(a.workgroups), dim3(S::kThreads), S::kLds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // the sequences' query heads fit the chip four waves each, or else a wave each
   if ((long long)a.n_q_heads * a.n_seqs * (D / kJoinChannels) <= 512)
-    hipLaunchKernelGGL(paged_join_many_kernel<D>, dim3(a.n_q_heads, a.n_seqs, D / kJoinChannels), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(paged_join_many_kernel<D>, dim3(a.n_q_heads, a.n_seqs, D / kJoinChannels), dim3(kJoinThreads), 0, s, a);
   else
-    hipLaunchKernelGGL(paged_join_kernel<D>, dim3((a.n_q_heads + kWaves - 1) / kWaves, a.n_seqs), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(paged_join_kernel<D>, dim3((a.n_q_heads + kJoinWaves - 1) / kJoinWaves, a.n_seqs), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
-constexpr int kCus = 256;
-static_assert(kCus * 4 <= kPagedMostWorkgroups, "room for the weights of pieces");
+template <int D, bool kE4m3>
+hipError_t prepare() {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(paged_decode_kernel<D, kE4m3, kAlone>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           Shape<D, kE4m3, kAlone>::kLds);
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(paged_decode_kernel<D, kE4m3, kShares>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             Shape<D, kE4m3, kShares>::kLds);
+}
 
 }  // namespace
 
 // as many as the chip holds at once
 int paged_decode_workgroups(int head_dim, bool e4m3) {
-  if (head_dim == 128) return kCus * (e4m3 ? Shape<128, true>::kPerCu : Shape<128, false>::kPerCu);
-  return kCus * (e4m3 ? Shape<64, true>::kPerCu : Shape<64, false>::kPerCu);
+  if (head_dim == 128) return kCus * (e4m3 ? Shape<128, true, kShares>::kPerCu : Shape<128, false, kShares>::kPerCu);
+  return kCus * (e4m3 ? Shape<64, true, kShares>::kPerCu : Shape<64, false, kShares>::kPerCu);
+}
+
+hipError_t prepare_paged_decode() {
+  hipError_t e;
+  if ((e = prepare<128, false>()) != hipSuccess || (e = prepare<128, true>()) != hipSuccess) return e;
+  if ((e = prepare<64, false>()) != hipSuccess) return e;
+  return prepare<64, true>();
 }
 
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s) {

@@ -1,5 +1,6 @@
 // Host side of the calls that serve many sequences at once: checks of the arguments and launches.  No state; no device memory is
 // allocated and no stream is synchronised.
+#include <atomic>
 #include <cmath>
 
 #include "serve.h"
@@ -70,14 +71,23 @@ int page_rows(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_b
   return code_of(write ? launch_page_write(a, pages->head_dim, e4m3, s) : launch_page_read(a, pages->head_dim, e4m3, s));
 }
 
+// Once per device: the attributes of functions, which belong to the current device (it is the stream's).
+int prepared() {
+  static std::atomic<unsigned long long> done{0};
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess) return KVP_EDEVICE;
+  const unsigned long long bit = device < 64 ? 1ull << device : 0;
+  if (done.load(std::memory_order_acquire) & bit) return KVP_OK;
+  if (prepare_paged_decode() != hipSuccess) return KVP_EDEVICE;
+  done.fetch_or(bit, std::memory_order_release);
+  return KVP_OK;
+}
+
 bool valid_group(int32_t n_q_heads, int32_t n_kv_heads) { return n_q_heads >= 1 && n_kv_heads >= 1 && n_q_heads % n_kv_heads == 0; }
 bool valid_scale(float s) { return s >= 0.f && !std::isinf(s); }
 float scale_log2_of(float scale, int head_dim) { return (scale > 0.f ? scale : 1.f / std::sqrt((float)head_dim)) * 1.4426950408889634f; }
 
 }  // namespace
-
-// Sequences that can have no more tiles than this (by the width of the table) are not cut into pieces.
-constexpr unsigned long long kPagedDirectTiles = 8;
 
 // What a decode step needs: two places for partial results per workgroup, each of a KV head's query heads.
 static size_t paged_decode_bytes(const kvp_pages& p, int group) {
@@ -101,6 +111,7 @@ int kvp_paged_decode(const kvp_pages* pages, const void* q, int64_t q_token, int
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lengths, 4) || !aligned(workspace, 16)) return KVP_EINVAL;
   if (!valid_strides(q_token, q_head) || !valid_scale(softmax_scale)) return KVP_EINVAL;
   if (workspace_bytes < kvp_paged_decode_bytes(pages, n_q_heads)) return KVP_ENOMEM;
+  if (const int rc = prepared()) return rc;
   PagedDecodeArgs a{};
   const bool e4m3 = pages->format == KVP_PAGE_E4M3;
   a.pool = pool_of(*pages);
@@ -112,7 +123,7 @@ int kvp_paged_decode(const kvp_pages* pages, const void* q, int64_t q_token, int
   a.width = table_width; a.n_seqs = n_seqs; a.n_q_heads = n_q_heads;
   a.group = n_q_heads / pages->n_kv_heads;
   a.workgroups = paged_decode_workgroups(pages->head_dim, e4m3);
-  a.direct = tiles <= kPagedDirectTiles ? 1 : 0;
+  a.most_keys = (long long)table_width * pages->page_size;
   a.by_heads = divisor_of((unsigned)pages->n_kv_heads, (unsigned)n_seqs * (unsigned)pages->n_kv_heads);
   a.by_group = divisor_of((unsigned)a.group, (unsigned)n_q_heads);
   a.scale_log2 = scale_log2_of(softmax_scale, pages->head_dim);

@@ -36,12 +36,13 @@ struct PagedDecodeArgs {
   long long q_token, q_head;
   int width, n_seqs, n_q_heads, group;
   int workgroups;
-  int direct;                 // one workgroup per sequence and KV head, nothing to join
+  long long most_keys;        // of a sequence, by the width of the table
   Divisor by_heads;           // n_heads of the pool
   Divisor by_group;
   float scale_log2;
 };
 constexpr int kPagedMostWorkgroups = 1024;
+hipError_t prepare_paged_decode();      // function attributes on the current device
 int paged_decode_workgroups(int head_dim, bool e4m3);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);
 

@@ -150,6 +150,37 @@ def test_rows_go_into_pages_and_come_back(e4m3, d, heads, page, how, lengths, fi
 
 
 @gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d,heads,n", [(128, 8, 5003), (64, 3, 22003), (128, 1, 33001)])
+def test_many_rows(d, heads, n, e4m3):
+    """More than the chip's waves take at once: several rows a wave, against the small calls that the other tests look at."""
+    gen = torch.Generator().manual_seed(n)
+    page, width = 64, -(-n // 64)
+    k, v = (numbers(gen, n, heads, d).to(DEV) for _ in range(2))
+    bounds = [0, 1, 1, n // 3, n - 700, n - 2]                                # the last two have no sequence
+    table = torch.randperm(5 * width, generator=gen).view(5, width).int().to(DEV)
+    first, many, few = int32([3, 0, 5, 0, 100]), *(a_pool(torch.Generator().manual_seed(1), 5 * width, heads, d, page, e4m3) for _ in range(2))
+    many.write(k, v, int32(bounds), table, first)
+    for s in range(5):
+        for t in range(bounds[s], bounds[s + 1], 2000):
+            m = min(2000, bounds[s + 1] - t)
+            few.write(k[t:t + m], v[t:t + m], int32([0, m]), table[s:s + 1], int32([int(first[s]) + t - bounds[s]]))
+    torch.cuda.synchronize()
+    for name in ("k", "v", "k_exp", "v_exp")[:4 if e4m3 else 2]:
+        assert torch.equal(getattr(many, name).view(torch.uint8), getattr(few, name).view(torch.uint8))
+    kr, vr = torch.full_like(k, 3.0), torch.full_like(v, 3.0)
+    many.read(kr, vr, int32(bounds), table, first)
+    torch.cuda.synchronize()
+    assert (kr[n - 2:] == 3).all() and (vr[n - 2:] == 3).all()
+    for s in range(5):
+        for t in range(bounds[s], bounds[s + 1], 2000):
+            m = min(2000, bounds[s + 1] - t)
+            ks, vs = torch.empty_like(k[:m]), torch.empty_like(v[:m])
+            few.read(ks, vs, int32([0, m]), table[s:s + 1], int32([int(first[s]) + t - bounds[s]]))
+            assert torch.equal(ks, kr[t:t + m]) and torch.equal(vs, vr[t:t + m])
+
+
+@gpu
 def test_e4m3_of_every_kind_of_row():
     """Every bf16 number, in rows whose largest magnitude is at most 2^r times theirs; zeros, infinities, NaNs; ties."""
     d, page = 64, 64
