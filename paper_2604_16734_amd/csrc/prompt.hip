@@ -39,8 +39,8 @@ struct Shape {
   static constexpr int kRowsPerLoad = 64 / kChunks;
   static constexpr int kLoads = kTileKeys / kWaves / kRowsPerLoad;      // of a wave, tensor and tile: 16 rows
   static constexpr int kTile = kTileKeys * D;                  // numbers
-  static constexpr int kLds = 4 * kTile * 2;
-  static_assert(kLds <= 64 * 1024, "LDS that a kernel has without asking");
+  static constexpr int kLds = 5 * kTile * 2;                   // two K, two V buffers, half of the query rows
+  static_assert(kPromptRows * D == 2 * kTile && 2 * kLds <= 160 * 1024, "two workgroups per CU");
 };
 
 // Tile of 128 rows number `rank` of a list of all sequences' tiles, those that see most keys first, so that the workgroups that come last are the
@@ -59,7 +59,7 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
     if (a.n_seqs <= 64) {
       if (__builtin_amdgcn_readlane(upto, 63) <= rank) break;
       // the t with  tiles from t + 1 on <= rank < tiles from t on
-      int lo = 0, hi = a.n_tokens / kPromptRows + 1, from_hi = 0;
+      int lo = 0, hi = __builtin_amdgcn_readfirstlane((int)over_wave((float)tiles, FloatMax{})), from_hi = 0;      // (below 2^24)
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2, n = sum_of_wave(max(tiles - mid, 0));
         if (n > rank) lo = mid;
@@ -173,8 +173,8 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
     for (int dt = 0; dt < kND; ++dt) v_off[dt] = rsub * D + 8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ z) + 4 * (lane & 1);
   }
 
-  // ---- the wave's query rows through a quarter of the buffers that are filled last, K's and V's second ones, beside tile 0
-  u16* const q_strip = (wave < 2 ? lds_k + S::kTile : lds_v + S::kTile) + (wave & 1) * 32 * D;
+  // ---- the wave's query rows, through the V buffer that is filled last and one like it; beside them the first tiles: one trip to memory for all
+  u16* const q_strip = lds_v + S::kTile + wave * 32 * D;
   {
     const int rows = min(32, n - q0);
     const u16* const at = q_rows + (long long)q0 * a.q_token;
@@ -193,6 +193,8 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
   load_tile(v_feed, v_lane, lds_dst(lds_v));
   move_on(k_feed);
   move_on(v_feed);
+  load_tile(k_feed, k_lane, lds_dst(lds_k + S::kTile));
+  move_on(k_feed);
 
   bf16x8 qf[kNK];                        // second operand: Q[q0 + l32][16 s + 8 g .. + 7]
   f32x16 o[kND], sx, sy;
@@ -203,14 +205,12 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
   for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
 #pragma unroll
   for (int r = 0; r < 8; ++r) px[r] = py[r] = 0u;
-  wait_all_but(std::integral_constant<int, S::kLoads>{});              // V(0) may still be on its way
+  wait_all_but(std::integral_constant<int, 2 * S::kLoads>{});          // V(0) and K(1) may still be on their way
 #pragma unroll
   for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(q_strip + k_off[st]);
 #pragma unroll
   for (int st = 0; st < kNK; ++st) asm volatile("" : "+v"(qf[st]));    // read, before the strip is filled again
   __syncthreads();
-  load_tile(k_feed, k_lane, lds_dst(lds_k + S::kTile));                // K(1)
-  move_on(k_feed);
   sx = zero;
 #pragma unroll
   for (int st = 0; st < kNK; ++st) sx = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_b128(lds_k + k_off[st]), qf[st], sx, 0, 0, 0);
@@ -453,6 +453,12 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
 }
 
 }  // namespace
+
+hipError_t prepare_prompt() {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<128>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<128>::kLds);
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<64>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<64>::kLds);
+}
 
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) {
   const dim3 grid(a.workgroups);

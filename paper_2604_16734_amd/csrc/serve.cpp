@@ -78,7 +78,7 @@ int prepared() {
   if (hipGetDevice(&device) != hipSuccess) return KVP_EDEVICE;
   const unsigned long long bit = device < 64 ? 1ull << device : 0;
   if (done.load(std::memory_order_acquire) & bit) return KVP_OK;
-  if (prepare_paged_decode() != hipSuccess) return KVP_EDEVICE;
+  if (prepare_paged_decode() != hipSuccess || prepare_prompt() != hipSuccess) return KVP_EDEVICE;
   done.fetch_or(bit, std::memory_order_release);
   return KVP_OK;
 }
@@ -152,6 +152,7 @@ int kvp_prompt_attention(const kvp_prompts* p, void* stream) {
   if (tiles * p->n_q_heads > (1ll << 30) - 64) return KVP_EINVAL;
   if (p->n_tokens == 0) return KVP_OK;
   if (!aligned(p->q, 16) || !aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->out, 16)) return KVP_EINVAL;
+  if (const int rc = prepared()) return rc;
   PromptArgs a{};
   a.q = static_cast<const u16*>(p->q);
   a.k = static_cast<const u16*>(p->k);

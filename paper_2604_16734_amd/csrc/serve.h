@@ -61,6 +61,7 @@ struct PromptArgs {
   Divisor by_set_heads, by_group;
   float scale_log2;
 };
+hipError_t prepare_prompt();            // function attributes on the current device
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s);
 
 hipError_t launch_page_write(const PageRowsArgs& a, int head_dim, bool e4m3, hipStream_t s);
