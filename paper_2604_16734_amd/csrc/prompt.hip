@@ -29,18 +29,23 @@
 namespace kvp {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kWaves = 4;              // of a workgroup, or of each half of one
 static_assert(kPromptRows == 32 * kWaves, "rows of a workgroup");
 constexpr int kTileKeys = 64;
 
-template <int D>
+// KS: groups of four waves that share the keys of the same rows, tile by tile in turns
+template <int D, int KS>
 struct Shape {
+  static constexpr int kThreads = 64 * kWaves * KS;
   static constexpr int kChunks = D / 8;                        // 16-byte chunks of a row
   static constexpr int kRowsPerLoad = 64 / kChunks;
   static constexpr int kLoads = kTileKeys / kWaves / kRowsPerLoad;      // of a wave, tensor and tile: 16 rows
   static constexpr int kTile = kTileKeys * D;                  // numbers
-  static constexpr int kLds = 5 * kTile * 2;                   // two K, two V buffers, half of the query rows
-  static_assert(kPromptRows * D == 2 * kTile && 2 * kLds <= 160 * 1024, "two workgroups per CU");
+  static constexpr int kGroupLds = 5 * kTile * 2;              // two K, two V buffers, half of the query rows
+  static constexpr int kLds = KS * kGroupLds;
+  static constexpr int kPerSimd = D == 64 && KS == 1 ? 3 : 2;  // waves
+  static_assert(kPromptRows * D == 2 * kTile && 2 * kGroupLds <= 160 * 1024, "two groups per CU");
+  static_assert(kPromptRows * D * 4 + 2 * kPromptRows * 4 <= kGroupLds, "what a group leaves for the first one");
 };
 
 // Tile of 128 rows number `rank` of a list of all sequences' tiles, those that see most keys first, so that the workgroups that come last are the
@@ -82,15 +87,15 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
   return PromptTile{0, 0, 0};
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(const PromptArgs a) {
-  using S = Shape<D>;
+template <int D, int KS>
+__global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerSimd)) prompt_kernel(const PromptArgs a) {
+  using S = Shape<D, KS>;
   constexpr int kNK = D / 16, kNV = (D / 32) * 2, kND = D / 32;       // K and V fragments of a block of 32 keys; channel tiles
   extern __shared__ __align__(16) unsigned char lds_raw[];
-  u16* const lds_k = reinterpret_cast<u16*>(lds_raw);              // [2][kTile]
-  u16* const lds_v = lds_k + 2 * S::kTile;                         // [2][kTile]
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int all_waves = __builtin_amdgcn_readfirstlane(tid >> 6), wave = all_waves % kWaves, ks = KS == 1 ? 0 : all_waves / kWaves;
+  u16* const lds_k = reinterpret_cast<u16*>(lds_raw + ks * S::kGroupLds);      // [2][kTile]
+  u16* const lds_v = lds_k + 2 * S::kTile;                                     // [2][kTile]
 
   // Dies and KV heads are dealt out to each other: dies_per_set dies share the query heads of as few KV heads as that allows, whose K and V
   // their L2 caches then hold, and take turns along the list of (tile, query head).
@@ -107,15 +112,18 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
   u16* const out_rows = a.out + pt.begin * a.out_token + h * a.out_head;
   const int q0 = wg_row + 32 * wave;                    // this wave's first row; it may lie past the end
   const int rows_end = min(n, wg_row + kPromptRows);
-  const int n_tiles = (rows_end + kTileKeys - 1) / kTileKeys;                              // of the workgroup
-  const int my_tiles = q0 < n ? (min(n, q0 + 32) + kTileKeys - 1) / kTileKeys : 0;        // that this wave sees
-  const int n_plain = min(my_tiles, (q0 + 1) / kTileKeys);                                // that all of its rows see whole
+  // tiles of a group: ks, ks + KS, ..
+  auto of_group = [&](int tiles, int which) __attribute__((always_inline)) { return (tiles - which + KS - 1) / KS; };
+  const int n_tiles = of_group((rows_end + kTileKeys - 1) / kTileKeys, 0);                 // steps of the workgroup
+  const int seen = q0 < n ? (min(n, q0 + 32) + kTileKeys - 1) / kTileKeys : 0;
+  const int my_tiles = of_group(seen, ks);                                                // that this wave sees
+  const int n_plain = of_group(min(seen, (q0 + 1) / kTileKeys), ks);                      // that all of its rows see whole
   const float sl2 = a.scale_log2;
 
   // ---- staging.  Wave w brings in rows 16 w .. 16 w + 15 of a tile; load j's immediate offset moves both of its addresses by 1 KiB, and the lane's part
   // takes that back where rows lie further apart.  (Inline assembly, and waits of this kernel's own: the compiler would have every read of
   // LDS wait for all loads.  s_nop: a load may read a scalar register five wait states after a vector instruction has written it.)
-  const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) void*)lds_raw);
+  const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) void*)lds_raw) + (unsigned)(ks * S::kGroupLds);
   auto lds_dst = [&](const u16* tile) __attribute__((always_inline)) -> unsigned {
     return lds_at + 2u * (unsigned)((int)(tile - lds_k) + 16 * wave * D);
   };
@@ -145,8 +153,8 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
                  : "m0", "memory");
   };
   auto move_on = [&](Feed& f) __attribute__((always_inline)) {
-    f.at += (unsigned long long)kTileKeys * f.row_bytes;
-    f.rows -= kTileKeys;
+    f.at += (unsigned long long)(KS * kTileKeys) * f.row_bytes;
+    f.rows -= KS * kTileKeys;
     f.bytes = bytes_of(f.rows, f.row_bytes);
   };
   auto load_tile = [&](const Feed& f, const unsigned (&of)[S::kLoads], unsigned to) __attribute__((always_inline)) {
@@ -188,7 +196,9 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of), "s"(buffer), "s"(to + 1024u * j) : "m0", "memory");
     }
   }
-  Feed k_feed = feed_at(k_rows, a.k_bytes, rows_end), v_feed = feed_at(v_rows, a.v_bytes, rows_end);
+  const int key0 = kTileKeys * ks;
+  Feed k_feed = feed_at(k_rows + (long long)key0 * a.k_token, a.k_bytes, rows_end - key0);
+  Feed v_feed = feed_at(v_rows + (long long)key0 * a.v_token, a.v_bytes, rows_end - key0);
   load_tile(k_feed, k_lane, lds_dst(lds_k));
   load_tile(v_feed, v_lane, lds_dst(lds_v));
   move_on(k_feed);
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
     u16* const k_nxt = lds_k + (buf ^ 1) * S::kTile;
     u16* const v_cur = lds_v + buf * S::kTile;
     u16* const v_prv = lds_v + (buf ^ 1) * S::kTile;
-    const int kb = t * kTileKeys;
+    const int kb = (KS * t + ks) * kTileKeys;
     prepare(sx, kb, mask, start);
     phase(sx, px, sy, k_cur + 32 * D, py, v_prv + 32 * D, std::integral_constant<bool, !kStart>{}, std::integral_constant<bool, !kStart>{}, No{}, nullptr,
           [](auto, int) {});
@@ -367,11 +377,35 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
   }
   wait_all_but(None{});
   __syncthreads();               // nothing is on its way into LDS, and nobody reads a tile any more
-  if (q0 >= n) return;
 #pragma unroll
   for (int dt = 0; dt < kND; ++dt) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[dt]));
-
   float l_row = sum_with_other_half(l_run);
+  if constexpr (KS == 2) {
+    // the second group leaves its rows as they lie in the accumulators, and the first one adds them up
+    float* const stat = reinterpret_cast<float*>(lds_raw + S::kGroupLds + kPromptRows * D * 4) + 64 * wave;       // [row, or 32 + row]
+    f32x4* const left = reinterpret_cast<f32x4*>(lds_raw + S::kGroupLds) + wave * 32 * D / 4 + lane;
+    auto four = [&](int k) __attribute__((always_inline)) -> f32x4 { return f32x4{o[k / 4][4 * (k % 4)], o[k / 4][4 * (k % 4) + 1], o[k / 4][4 * (k % 4) + 2], o[k / 4][4 * (k % 4) + 3]}; };
+    if (ks == 1) {
+#pragma unroll
+      for (int k = 0; k < 4 * kND; ++k) left[64 * k] = four(k);
+      if (g == 0) {
+        stat[l32] = m_ref;
+        stat[32 + l32] = l_row;
+      }
+    }
+    __syncthreads();
+    if (ks == 1) return;
+    const float m_other = stat[l32], top = fmaxf(m_ref, m_other), use = top == -INFINITY ? 0.f : top;
+    const float f0 = __builtin_amdgcn_exp2f((m_ref - use) * sl2), f1 = __builtin_amdgcn_exp2f((m_other - use) * sl2);
+    l_row = l_row * f0 + stat[32 + l32] * f1;
+#pragma unroll
+    for (int k = 0; k < 4 * kND; ++k) {
+      const f32x4 x = left[64 * k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[k / 4][4 * (k % 4) + e] = o[k / 4][4 * (k % 4) + e] * f0 + x[e] * f1;
+    }
+  }
+  if (q0 >= n) return;
   // what is not finite is not 0 when it is multiplied by 0
   float check = 0.f;
 #pragma unroll
@@ -454,17 +488,31 @@ __global__ void __launch_bounds__(kThreads, (D == 64 ? 3 : 2)) prompt_kernel(con
 
 }  // namespace
 
+namespace {
+template <int D, int KS>
+hipError_t prepare() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<D, KS>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<D, KS>::kLds);
+}
+template <int D, int KS>
+hipError_t launch(const PromptArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((prompt_kernel<D, KS>), dim3(a.workgroups), dim3(Shape<D, KS>::kThreads), (Shape<D, KS>::kLds), s, a);
+  return hipGetLastError();
+}
+}  // namespace
+
 hipError_t prepare_prompt() {
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<128>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<128>::kLds);
-  if (e != hipSuccess) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<64>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<64>::kLds);
+  hipError_t e;
+  if ((e = prepare<128, 1>()) != hipSuccess || (e = prepare<128, 2>()) != hipSuccess || (e = prepare<64, 1>()) != hipSuccess) return e;
+  return prepare<64, 2>();
 }
 
+// Two groups of waves share the keys where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of the
+// time) and the prompts are not too short for it.  One prompt of 32/8 heads, one group and two: d 128, 128 rows 6.5 and 7.6 us, 256 8.6 and 8.9, 512 12.3 and
+// 11.9, 2000 rows of 8/2 heads 30.2 and 25.9; d 64, 256 rows 6.8 and 6.6, 512 9.4 and 8.5, 1024 15.2 and 12.6.
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) {
-  const dim3 grid(a.workgroups);
-  if (head_dim == 128) hipLaunchKernelGGL(prompt_kernel<128>, grid, dim3(kThreads), Shape<128>::kLds, s, a);
-  else hipLaunchKernelGGL(prompt_kernel<64>, grid, dim3(kThreads), Shape<64>::kLds, s, a);
-  return hipGetLastError();
+  const bool few = a.workgroups <= 256 && a.n_tokens >= 384ll * a.n_seqs;
+  if (head_dim == 128) return few ? launch<128, 2>(a, s) : launch<128, 1>(a, s);
+  return few ? launch<64, 2>(a, s) : launch<64, 1>(a, s);
 }
 
 }  // namespace kvp

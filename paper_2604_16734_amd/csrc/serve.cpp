@@ -148,7 +148,7 @@ int kvp_prompt_attention(const kvp_prompts* p, void* stream) {
     if (!valid_strides(s[0], s[1]) || (p->n_tokens > 1 && s[0] < p->head_dim)) return KVP_EINVAL;
   if (!separate_rows(p->out_token, p->out_head, p->n_tokens, p->n_q_heads, p->head_dim)) return KVP_EINVAL;
   // tiles of rows, at most: every prompt may have one that is not full
-  const long long tiles = (long long)p->n_tokens / kPromptRows + p->n_seqs;
+  const long long tiles = ((long long)p->n_tokens + (long long)(kPromptRows - 1) * p->n_seqs) / kPromptRows;
   if (tiles * p->n_q_heads > (1ll << 30) - 64) return KVP_EINVAL;
   if (p->n_tokens == 0) return KVP_OK;
   if (!aligned(p->q, 16) || !aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->out, 16)) return KVP_EINVAL;
