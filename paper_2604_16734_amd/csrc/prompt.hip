@@ -357,13 +357,35 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
       body(t, Odd{}, No{}, No{});
       body(t + 1, Even{}, No{}, No{});
     }
-    for (; t < my_tiles; ++t) body(t, Any{}, No{}, Yes{});       // (a mask does nothing to a tile that is seen whole)
-    // O += P_Y V of the last tile: its V is there since the barrier inside the last body, until the next one
-    const u16* const vt = lds_v + ((my_tiles + 1) & 1) * S::kTile + 32 * D;
+    // the last tile of them all has the diagonal: in its first block, and then nobody sees the second one, or in the second
+    const bool half = KS * (my_tiles - 1) + ks == seen - 1 && q0 % kTileKeys == 0 && t < my_tiles;
+    for (; t < my_tiles - half; ++t) body(t, Any{}, No{}, Yes{});       // (a mask does nothing to a tile that is seen whole)
+    auto add_values = [&](const unsigned (&p)[8], const u16* vt) __attribute__((always_inline)) {
 #pragma unroll
-    for (int vi = 0; vi < kNV; ++vi) {
-      const u32x4 pw = {py[4 * (vi % 2)], py[4 * (vi % 2) + 1], py[4 * (vi % 2) + 2], py[4 * (vi % 2) + 3]};
-      o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_vt(vt + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D), __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
+      for (int vi = 0; vi < kNV; ++vi) {
+        const u32x4 pw = {p[4 * (vi % 2)], p[4 * (vi % 2) + 1], p[4 * (vi % 2) + 2], p[4 * (vi % 2) + 3]};
+        o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_vt(vt + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D), __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
+      }
+    };
+    // O += P_Y V of the last tile: its V is there since the barrier inside the last body, until the next one
+    add_values(py, lds_v + ((t & 1) ^ 1) * S::kTile + 32 * D);
+    if (half) {
+      prepare(sx, (KS * t + ks) * kTileKeys, Yes{}, No{});
+      const float neg = m_ref == -INFINITY ? 0.f : -m_ref * sl2;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[r], sl2, neg)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[r + 1], sl2, neg));
+        l_run += p0 + p1;
+        px[r / 2] = pack_bf16(p0, p1);
+      }
+      wait_all_but(None{});
+      __syncthreads();
+      load_tile(k_feed, k_lane, lds_dst(lds_k + (t & 1) * S::kTile));
+      load_tile(v_feed, v_lane, lds_dst(lds_v + ((t & 1) ^ 1) * S::kTile));
+      move_on(k_feed);
+      move_on(v_feed);
+      add_values(px, lds_v + (t & 1) * S::kTile);
+      ++t;
     }
   }
   // tiles that only later rows of the workgroup see: in step with their waves
