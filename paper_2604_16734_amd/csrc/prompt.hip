@@ -63,6 +63,10 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
     const int upto = sum_upto(tiles);
     if (a.n_seqs <= 64) {
       if (__builtin_amdgcn_readlane(upto, 63) <= rank) break;
+      if (a.n_seqs == 1) {
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        return PromptTile{__builtin_amdgcn_readlane(begin, 0), __builtin_amdgcn_readlane(end - begin, 0), all - 1 - rank};
+      }
       // the t with  tiles from t + 1 on <= rank < tiles from t on
       int lo = 0, hi = __builtin_amdgcn_readfirstlane((int)over_wave((float)tiles, FloatMax{})), from_hi = 0;      // (below 2^24)
       while (hi - lo > 1) {
@@ -259,6 +263,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
     auto read_v = [&](int vi) __attribute__((always_inline)) { vfr[vi] = lds_read_vt(vt + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D); };
     int ei = 0;
     float arg = __builtin_fmaf(s_exp[0], sl2, neg), pe1 = 0.f, pe2 = 0.f;
+    // (sums of the packed weights, two to an instruction by v_dot2_f32_bf16: 6 % slower)
     auto finish_element = [&](int e) __attribute__((always_inline)) {
       sum += pe1;
       asm volatile("" : "+v"(sum));          // (left alone the compiler gathers the additions of several phases in one place)
@@ -399,8 +404,8 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   }
   wait_all_but(None{});
   __syncthreads();               // nothing is on its way into LDS, and nobody reads a tile any more
-#pragma unroll
-  for (int dt = 0; dt < kND; ++dt) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[dt]));
+  if constexpr (kND == 4) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]));       // (as after the first products)
+  else asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]));
   float l_row = sum_with_other_half(l_run);
   if constexpr (KS == 2) {
     // the second group leaves its rows as they lie in the accumulators, and the first one adds them up
@@ -429,12 +434,14 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   }
   if (q0 >= n) return;
   // what is not finite is not 0 when it is multiplied by 0
-  float check = 0.f;
+  float check[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int dt = 0; dt < kND; ++dt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[dt][r], 0.f, check);
-  if (__any(!(l_row <= 0x1p64f) || !(check == 0.f))) {
+    for (int r = 0; r < 16; ++r) check[r % 8] = __builtin_fmaf(o[dt][r], 0.f, check[r % 8]);
+  check[0] += check[1] + check[2] + check[3];
+  check[4] += check[5] + check[6] + check[7];
+  if (__any(!(l_row <= 0x1p64f) || !(check[0] + check[4] == 0.f))) {
     // ---- the slow way: running maximum, one block of 32 keys at a time straight from memory
     float m_run = -INFINITY;
     l_row = 0.f;
