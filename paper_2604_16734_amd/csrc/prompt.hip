@@ -536,10 +536,12 @@ hipError_t prepare_prompt() {
 }
 
 // Two groups of waves share the keys where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of the
-// time) and the prompts are not too short for it.  One prompt of 32/8 heads, one group and two: d 128, 128 rows 6.5 and 7.6 us, 256 8.6 and 8.9, 512 12.3 and
-// 11.9, 2000 rows of 8/2 heads 30.2 and 25.9; d 64, 256 rows 6.8 and 6.6, 512 9.4 and 8.5, 1024 15.2 and 12.6.
+// time), or nearly so and the longest of them decides, and the prompts are not too short for it.  One prompt of 32/8 heads, one group and two: d 128, 128 rows
+// 6.5 and 7.6 us, 256 8.6 and 8.9, 512 12.3 and 11.9, 1536 30.3 and 27.4, 4096 132 and 136, 8000 rows of 8/2 heads (504 workgroups) 138 and 122, 16000 of 4/4 (500)
+// 270 and 233; d 64, 256 rows 6.8 and 6.6, 512 9.4 and 8.5, 1024 15.2 and 12.6, 16000 of 4/4 170 and 150.  8 prompts of 500 rows, 16/4 heads, d 128, 18.0 and 23.7.
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) {
-  const bool few = a.workgroups <= 256 && a.n_tokens >= 384ll * a.n_seqs;
+  const long long mean = a.n_tokens / a.n_seqs;
+  const bool few = (a.workgroups <= 256 && mean >= 384) || (a.workgroups <= 512 && mean >= 1024);
   if (head_dim == 128) return few ? launch<128, 2>(a, s) : launch<128, 1>(a, s);
   return few ? launch<64, 2>(a, s) : launch<64, 1>(a, s);
 }

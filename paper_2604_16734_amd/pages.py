@@ -114,10 +114,26 @@ class Pages:
         self.of = KvpPages(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if e4m3 else None, v_exp.data_ptr() if e4m3 else None,
                            KVP_PAGE_E4M3 if e4m3 else KVP_PAGE_BF16, *k.shape)
         self._ref, self._lib = ctypes.byref(self.of), lib()
-        # what every call needs, looked up once (a step of a few sequences takes the GPU 4 us; through Python alone a call took the host 8)
-        self._at, self._index = ctypes.addressof(self.of), k.device.index
-        self._native_rows, self._native_decode = _fast_call("page_rows"), _fast_call("paged_decode")
-        self._device, self._stream, self._work = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, {}
+        # what every call needs, looked up once (rows of a few sequences take the GPU 2.6 us; through Python alone a call took the host 8)
+        native = _fast_call("page_rows"), _fast_call("paged_decode")
+        device, stream, index = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, k.device.index
+        at, heads, dim, work = ctypes.addressof(self.of), self.n_kv_heads, self.head_dim, {}
+        rows, decode, write_entry, read_entry, decode_entry = *native, _entries.kvp_page_write, _entries.kvp_page_read, _entries.kvp_paged_decode
+        self._work = work
+
+        def native_write(k, v, seq_begin, table, first):
+            if device() == index:
+                return rows(write_entry, at, heads, dim, index, stream(index), k, v, seq_begin, table, first)
+
+        def native_read(k, v, seq_begin, table, first):
+            if device() == index:
+                return rows(read_entry, at, heads, dim, index, stream(index), k, v, seq_begin, table, first)
+
+        def native_decode(q, n_q_heads, table, lengths, out, workspace, softmax_scale):
+            if device() == index:
+                return decode(decode_entry, at, n_q_heads, dim, index, stream(index), q, table, lengths, out, workspace, softmax_scale)
+
+        self._native_write, self._native_read, self._native_decode = native_write, native_read, native_decode
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, page_size=64, e4m3=False, device="cuda:0"):
@@ -130,13 +146,6 @@ class Pages:
         return cls(new(shape, torch.float8_e4m3fn), new(shape, torch.float8_e4m3fn), new(shape[:3], torch.uint8), new(shape[:3], torch.uint8))
 
     def _rows(self, call, k, v, seq_begin, table, first, stream):
-        if stream is None and self._device() == self._index:
-            rc = self._native_rows(getattr(_entries, "kvp_page_" + call), self._at, self.n_kv_heads, self.head_dim, self._index, self._stream(self._index),
-                                   k, v, seq_begin, table, first)
-            if rc == 0:
-                return
-            if rc is not None:
-                raise KvpError(rc, "kvp_page_" + call)
         n_tokens, n_seqs, device = k.shape[0], seq_begin.numel() - 1, self.device
         what = "Pages.%s: " % call
         shape = (n_tokens, self.n_kv_heads, self.head_dim)
@@ -155,11 +164,19 @@ class Pages:
     def write(self, k, v, seq_begin, table, first=None, stream=None):
         """Rows seq_begin[s] .. seq_begin[s + 1] - 1 of k and v [n_tokens, n_kv_heads, head_dim] (any strides but the last) become
         tokens first[s], first[s] + 1, ... of sequence s, whose pages are table[s] (kvp_page_write)."""
-        self._rows("write", k, v, seq_begin, table, first, stream)
+        rc = self._native_write(k, v, seq_begin, table, first) if stream is None else None
+        if rc is None:
+            self._rows("write", k, v, seq_begin, table, first, stream)
+        elif rc:
+            raise KvpError(rc, "kvp_page_write")
 
     def read(self, k, v, seq_begin, table, first=None, stream=None):
         """The way back, into k and v (kvp_page_read)."""
-        self._rows("read", k, v, seq_begin, table, first, stream)
+        rc = self._native_read(k, v, seq_begin, table, first) if stream is None else None
+        if rc is None:
+            self._rows("read", k, v, seq_begin, table, first, stream)
+        elif rc:
+            raise KvpError(rc, "kvp_page_read")
 
     def _workspace_bytes(self, n_q_heads):
         nbytes = self._work.get(n_q_heads)
@@ -177,18 +194,17 @@ class Pages:
         """One token of every sequence: q [n_seqs, n_q_heads, head_dim] over tokens 0 .. lengths[s] - 1 of the pages table[s]
         (kvp_paged_decode).  Without a workspace one is allocated for the call."""
         import torch
-        n_seqs, device = lengths.numel(), self.device
-        _need(q.dim() == 3 and table.dim() == 2, "Pages.decode: q and table")
-        n_q_heads, what = q.shape[1], "Pages.decode: "
-        if stream is None and self._device() == self._index:
-            if out is None:
-                out = torch.empty((n_seqs, n_q_heads, self.head_dim), dtype=torch.bfloat16, device=device)
-            rc = self._native_decode(_entries.kvp_paged_decode, self._at, n_q_heads, self.head_dim, self._index, self._stream(self._index), q, table, lengths,
-                                     out, self._workspace_bytes(n_q_heads) if workspace is None else workspace, softmax_scale)
+        if stream is None and out is not None:
+            n_q_heads = q.shape[-2] if q.dim() > 1 else 0
+            room = workspace if workspace is not None else self._work.get(n_q_heads) or self._workspace_bytes(n_q_heads)
+            rc = self._native_decode(q, n_q_heads, table, lengths, out, room, softmax_scale)
             if rc == 0:
                 return out
             if rc is not None:
                 raise KvpError(rc, "kvp_paged_decode")
+        n_seqs, device = lengths.numel(), self.device
+        _need(q.dim() == 3 and table.dim() == 2, "Pages.decode: q and table")
+        n_q_heads, what = q.shape[1], "Pages.decode: "
         shape = (n_seqs, n_q_heads, self.head_dim)
         q_at, q_token, q_head = _numbers(q, shape, device, what + "q")
         table_at = _whole(table, (n_seqs, table.shape[1]), device, what + "table")
