@@ -4,12 +4,12 @@
 // Bound by HBM: every key and value is read once and meets the G query heads of its KV head, 4 G flops for two numbers.  So what counts is
 // that every CU has loads on their way all the time, and that none of them has more to do than the others.
 //
-// Who does what.  The lengths are on the device, and the host plans nothing: pages.h deals the units of all sequences, tiles of 128 keys of
+// Who does what.  The lengths are on the device, and the host plans nothing: pages.h deals the units of all sequences, tiles of 256 keys of
 // one KV head, to a fixed number of workgroups, as many as the chip holds at once, in equal shares; a workgroup finds its share by adding up the
 // lengths.  A piece that is all of a sequence and head is finished at once; the partial results (maximum, sum, unscaled output) of the others go
 // to the workspace, and a second kernel joins them, in the order of the workgroups, so that the same input gives the same bits.
 //
-// Within a tile each of the four waves takes 32 keys by itself, through two strips of LDS of its own, one for K and one for V: the next
+// Within a tile each of the eight waves takes 32 keys by itself, through two strips of LDS of its own, one for K and one for V: the next
 // tile's K is on its way as soon as this one's has been read, and the same for V; no barrier until a piece is done.  The rows come by
 // buffer_load ... lds, 16 at a time (no page is shorter), through descriptors that end with the last row there is: rows behind a
 // sequence's end, and of pages that do not exist, come as zeros without being read.
@@ -29,17 +29,16 @@ namespace {
 
 constexpr int kKeys = 32;                      // keys of a wave's part of a tile: two blocks of 16
 constexpr int kHeads = 16;                     // columns of the products
-constexpr int kAloneWaves = 8;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+static_assert(kKeys * kWaves == kPagedTile, "tiles of pages.h");
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 // Ways to spread the work: in shares, as above; or a workgroup for every sequence and KV head, with nothing to join.
 enum Way { kShares, kAlone };
 
-template <int D, bool kE4m3, Way kWay>
+template <int D, bool kE4m3>
 struct Shape {
-  static constexpr int kWaves = kWay == kShares ? kPagedTile / kKeys : kAloneWaves;
-  static constexpr int kThreads = 64 * kWaves, kTile = kKeys * kWaves;
   static constexpr int kRow = kE4m3 ? D : 2 * D;                  // bytes of a row in the pages
   static constexpr int kChunks = kRow / 16;
   static constexpr int kLoads = kRow / 64;                        // of 1 KiB, for 16 rows
@@ -47,7 +46,7 @@ struct Shape {
   static constexpr int kExps = kE4m3 ? 256 : 0;
   static constexpr int kWaveBytes = 2 * kStrip + kExps;           // K, V, exponents
   static constexpr int kLds = kWaves * kWaveBytes;
-  static constexpr int kPerCu = kLds > 80 * 1024 ? 1 : kLds > 40 * 1024 || kWaves == 8 ? 2 : 4;      // workgroups of a CU
+  static constexpr int kPerCu = kLds > 80 * 1024 ? 1 : 2;         // workgroups of a CU
   // what a wave leaves of a piece lies over its strips: the output as it is in the accumulators, then maxima and sums
   static constexpr int kOut = kHeads * D * 4, kStat = kE4m3 ? 2 * kStrip : kOut;
   static_assert(kOut <= 2 * kStrip && kStat + 2 * kHeads * 4 <= kWaveBytes, "room for a piece");
@@ -91,11 +90,10 @@ __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, int seq) {
 }
 // Not in shares: workgroup b has all of sequence b / n_heads, KV head b % n_heads, and there is nothing to join.
 template <int D, bool kE4m3, Way kWay>
-__global__ void __launch_bounds__((Shape<D, kE4m3, kWay>::kThreads), (Shape<D, kE4m3, kWay>::kPerCu * Shape<D, kE4m3, kWay>::kWaves / 4))
+__global__ void __launch_bounds__(kThreads, 4)
 paged_decode_kernel(const PagedDecodeArgs a) {
-  using S = Shape<D, kE4m3, kWay>;
+  using S = Shape<D, kE4m3>;
   constexpr bool kDirect = kWay == kAlone;
-  constexpr int kWaves = S::kWaves, kThreads = S::kThreads, kTile = S::kTile;
   constexpr int kRow = S::kRow, kChunks = S::kChunks, kLoads = S::kLoads;
   constexpr int kSteps = D / 32;                 // products with K of a block of 16 keys
   constexpr int kTiles = D / 16;                 // channel tiles of the output
@@ -219,7 +217,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       seq_end = before + (unsigned)__builtin_amdgcn_readlane((int)upto, i);
       seq_first = seq_end - (unsigned)__builtin_amdgcn_readlane((int)tiles, i);
     }
-    const unsigned n_tiles = (unsigned)(n_keys + kTile - 1) / kTile;
+    const unsigned n_tiles = (unsigned)paged_tiles(n_keys);
     const int head = kDirect ? direct_head : __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
     const unsigned first = seq_first + (unsigned)head * n_tiles;      // the first unit of this sequence and head
     const int t0 = kDirect ? 0 : (int)(at - first), t1 = kDirect ? (int)n_tiles : (int)(min(end, first + n_tiles) - first);
@@ -237,7 +235,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       ids = col + lane < a.width ? row_of_table[col + lane] : -1;
       rows_of_ids();
     };
-    const int kb0 = kTile * t0 + kKeys * wave;
+    const int kb0 = kPagedTile * t0 + kKeys * wave;
     if (kDirect) rows_of_ids();
     else if (kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
 
@@ -261,9 +259,9 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       int rows[2];
       long long at[2];
     };
-    const int my_end = min(t1, (n_keys - kKeys * wave + kTile - 1) / kTile);      // tiles in which this wave has keys
+    const int my_end = min(t1, (n_keys - kKeys * wave + kPagedTile - 1) / kPagedTile);      // tiles in which this wave has keys
     auto tile_at = [&](int t) __attribute__((always_inline)) -> Tile {
-      const int kb = kTile * t + kKeys * wave;
+      const int kb = kPagedTile * t + kKeys * wave;
       Tile x;
       if (((kb + 16) >> a.pool.shift) - col0 >= 64) load_ids(kb >> a.pool.shift);
 #pragma unroll
@@ -571,22 +569,22 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const Pag
 }
 
 constexpr int kCus = 256;
-static_assert(kCus * 4 <= kPagedMostWorkgroups, "room for the weights of pieces");
+static_assert(kCus * 2 <= kPagedMostWorkgroups, "room for the weights of pieces");
 // A workgroup of its own for every sequence and KV head: where no sequence can have more keys than this, by the width of the table; more
-// where there are so many that all CUs have one.  8 KV heads, d 128, e4m3, alone and in shares: one sequence of 512 keys 5.8 and 8.1 us, 768 7.0
-// and 8.2, 1024 8.9 and 8.2; 32 sequences of 512 7.2 and 13.0, of 1000 13.4 and 18.5, of 2500 27.1 and 32.0, of 2500 once and 300 else 15.6 and 13.8.
+// where there are so many that all CUs have one.  8 KV heads, d 128, e4m3, alone and in shares: one sequence of 512 keys 5.9 and 8.6 us, 768 7.4
+// and 8.6, 1024 8.9 and 8.7; 32 sequences of 512 7.2 and 12.2, of 1000 13.4 and 17.7, of 2500 27.4 and 32.3, of 44 to 2176 14.4 and 16.3; of 2500 once and
+// 300 else 15.4 and 11.8.
 constexpr long long kAloneKeys = 768, kAloneKeysOfMany = 2560;
 
 template <int D, bool kE4m3>
 hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {
+  using S = Shape<D, kE4m3>;
   const unsigned pairs = (unsigned)a.n_seqs * (unsigned)a.pool.n_heads;
   if (a.most_keys <= (pairs >= kCus ? kAloneKeysOfMany : kAloneKeys)) {
-    using S = Shape<D, kE4m3, kAlone>;
-    hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kAlone>), dim3(pairs), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kAlone>), dim3(pairs), dim3(kThreads), S::kLds, s, a);
     return hipGetLastError();
   }
-  using S = Shape<D, kE4m3, kShares>;
-  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kShares>), dim3(a.workgroups), dim3(S::kThreads), S::kLds, s, a);
+  hipLaunchKernelGGL((paged_decode_kernel<D, kE4m3, kShares>), dim3(a.workgroups), dim3(kThreads), S::kLds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // the sequences' query heads fit the chip four waves each, or else a wave each
@@ -600,18 +598,18 @@ hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {
 template <int D, bool kE4m3>
 hipError_t prepare() {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(paged_decode_kernel<D, kE4m3, kAlone>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           Shape<D, kE4m3, kAlone>::kLds);
+                                           Shape<D, kE4m3>::kLds);
   if (e != hipSuccess) return e;
   return hipFuncSetAttribute(reinterpret_cast<const void*>(paged_decode_kernel<D, kE4m3, kShares>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             Shape<D, kE4m3, kShares>::kLds);
+                             Shape<D, kE4m3>::kLds);
 }
 
 }  // namespace
 
 // as many as the chip holds at once
 int paged_decode_workgroups(int head_dim, bool e4m3) {
-  if (head_dim == 128) return kCus * (e4m3 ? Shape<128, true, kShares>::kPerCu : Shape<128, false, kShares>::kPerCu);
-  return kCus * (e4m3 ? Shape<64, true, kShares>::kPerCu : Shape<64, false, kShares>::kPerCu);
+  if (head_dim == 128) return kCus * (e4m3 ? Shape<128, true>::kPerCu : Shape<128, false>::kPerCu);
+  return kCus * (e4m3 ? Shape<64, true>::kPerCu : Shape<64, false>::kPerCu);
 }
 
 hipError_t prepare_paged_decode() {

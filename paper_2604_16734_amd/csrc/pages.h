@@ -30,7 +30,7 @@ KVP_HOST_DEVICE int e4m3_exponent(unsigned bf16_magnitude) {
 // and heads they belong to: every workgroup has the same work, however the lengths are spread, and the host needs to know none of them.  The
 // units of one sequence and head in one workgroup are a piece.  A workgroup has one piece at most that another workgroup's goes before (its
 // first) and one that another's follows (its last, perhaps the same); every other is whole, and its result final.
-constexpr int kPagedTile = 128;
+constexpr int kPagedTile = 256;
 
 KVP_HOST_DEVICE int paged_tiles(int length) { return (int)(((unsigned)length + kPagedTile - 1) / kPagedTile); }
 // units of a workgroup

@@ -41,7 +41,7 @@ struct PagedDecodeArgs {
   Divisor by_group;
   float scale_log2;
 };
-constexpr int kPagedMostWorkgroups = 1024;
+constexpr int kPagedMostWorkgroups = 512;
 hipError_t prepare_paged_decode();      // function attributes on the current device
 int paged_decode_workgroups(int head_dim, bool e4m3);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);

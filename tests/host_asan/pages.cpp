@@ -35,8 +35,8 @@ int main() {
   // rows of the last page of a pool beyond 32 bits
   if (kvp::page_row(2147483646, 64, 63, 255, 8) != ((2147483646ull * 64 + 63) << 8) + 255) return fail("row", 0, 0, 0);
 
-  for (int length : {0, 1, 127, 128, 129, 1 << 30})
-    if (kvp::paged_tiles(length) != (length + 127LL) / 128) return fail("tiles", length, kvp::paged_tiles(length), 0);
+  for (int length : {0, 1, 127, 128, 129, 255, 256, 257, 1 << 30})
+    if (kvp::paged_tiles(length) != (length + kvp::kPagedTile - 1LL) / kvp::kPagedTile) return fail("tiles", length, kvp::paged_tiles(length), 0);
   uint64_t seed = 1;
   auto below = [&](unsigned n) { seed = seed * 6364136223846793005ull + 1442695040888963407ull; return (unsigned)((seed >> 33) % n); };
   for (int trial = 0; trial < 3000; ++trial) {

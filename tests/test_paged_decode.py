@@ -130,6 +130,29 @@ def test_many_sequences(e4m3):
 
 @gpu
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("hq,hkv,d,page,lengths", [
+    (32, 32, 64, 16, [2001, 1, 0, 700, 33, 2500, 16, 129]),                   # a workgroup each, more than 64 columns of the table
+    (16, 16, 128, 64, [2500] + [37 * i % 900 for i in range(17)]),
+    (32, 2, 64, 64, [60001] + [11 * i for i in range(39)]),                   # many sequences, one of them in hundreds of pieces
+    (8, 1, 128, 256, [30000, 0, 1, 257]),                                     # few
+])
+def test_every_way_to_spread_the_work(hq, hkv, d, page, lengths, e4m3):
+    gen = torch.Generator().manual_seed(hq + page)
+    pages, table = a_batch(gen, lengths, hkv, d, page, e4m3)
+    q = (2 * torch.randn(len(lengths), hq, d, generator=gen)).to(torch.bfloat16)
+    print("paged decode, ways", hq, hkv, d, page, len(lengths), e4m3, flush=True)
+    out = pages.decode(q.to(DEV), table, int32(lengths), workspace=pages.workspace(hq).fill_(0xFF))
+    wide = torch.full((len(lengths), 2 * table.shape[1] + 200), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table                                          # the same under a table that says less
+    again = pages.decode(q.to(DEV), wide, int32(lengths))
+    torch.cuda.synchronize()
+    ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, page, d ** -0.5)
+    check(out, ref, size, most, d)
+    check(again, ref, size, most, d)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_a_long_sequence_and_the_same_bits_again(e4m3):
     """All workgroups on the pieces of one sequence; large logits, the largest of them last."""
     gen = torch.Generator().manual_seed(9)

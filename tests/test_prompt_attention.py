@@ -70,7 +70,7 @@ def test_against_64_bits(hq, hkv, d, lengths):
 
 
 @gpu
-@pytest.mark.parametrize("hq,hkv,d,n", [(8, 2, 128, 4097), (2, 1, 64, 5000), (1, 1, 128, 9001)])
+@pytest.mark.parametrize("hq,hkv,d,n", [(8, 2, 128, 4097), (2, 1, 64, 5000), (1, 1, 128, 9001), (24, 8, 64, 2900), (20, 4, 128, 3500)])
 def test_long_prompts(hq, hkv, d, n):
     gen = torch.Generator().manual_seed(n)
     q, k, v = randn(gen, n, hq, d, scale=2.0), randn(gen, n, hkv, d), randn(gen, n, hkv, d)
