@@ -449,7 +449,7 @@ int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* s
  * Query head h reads KV head h / (n_q_heads / n_kv_heads).  fp32 accumulation, rounded
  * once; softmax_scale 0 means 1/sqrt(head_dim).  What a row does not see has no part in
  * it, were it infinite.  n_tokens = 0 does nothing.  KVP_EINVAL also where
- * (n_tokens / 128 + n_seqs) * n_q_heads passes 2^30 - 64, or rows from token to token are
+ * (n_tokens / 32 + n_seqs) * n_q_heads passes 2^30 - 64, or rows from token to token are
  * less than head_dim apart. */
 typedef struct kvp_prompts {
   const void* q;

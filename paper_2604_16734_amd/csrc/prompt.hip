@@ -48,18 +48,19 @@ struct Shape {
   static_assert(kPromptRows * D * 4 + 2 * kPromptRows * 4 <= kGroupLds, "what a group leaves for the first one");
 };
 
-// Tile of 128 rows number `rank` of a list of all sequences' tiles, those that see most keys first, so that the workgroups that come last are the
+// Tile of kRows rows number `rank` of a list of all sequences' tiles, those that see most keys first, so that the workgroups that come last are the
 // short ones: tile t of a sequence comes before all tiles t - 1.  With more than 64 sequences the list goes through the sequences instead, each
 // one's last tile first: a look at all of them for every step of the search would take longer than it saves.
 struct PromptTile {
   int begin, length, tile;            // the sequence's first row and its rows; length 0: no such tile
 };
+template <int kRows>
 __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, int lane) {
   int before = 0;
   for (int base = 0; base < a.n_seqs; base += 64) {
     const int s = min(base + lane, a.n_seqs - 1);
     const int begin = min(max(a.seq_begin[s], 0), a.n_tokens), end = min(max(a.seq_begin[s + 1], begin), a.n_tokens);
-    const int tiles = base + lane < a.n_seqs ? (end - begin + kPromptRows - 1) / kPromptRows : 0;
+    const int tiles = base + lane < a.n_seqs ? (end - begin + kRows - 1) / kRows : 0;
     const int upto = sum_upto(tiles);
     if (a.n_seqs <= 64) {
       if (__builtin_amdgcn_readlane(upto, 63) <= rank) break;
@@ -91,6 +92,83 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
   return PromptTile{0, 0, 0};
 }
 
+// Dies and KV heads are dealt out to each other: dies_per_set dies share the query heads of as few KV heads as that allows, whose K and V
+// their L2 caches then hold, and take turns along the list of (tile, query head).
+struct Item {
+  int rank, head;
+};
+__device__ __forceinline__ Item item_of(const PromptArgs& a) {
+  const int xcd = blockIdx.x % kXcds, set = xcd / a.dies_per_set;
+  const unsigned item = blockIdx.x / kXcds * (unsigned)a.dies_per_set + (unsigned)(xcd - set * a.dies_per_set);
+  const int rank = (int)quotient(item, a.by_set_heads);
+  return Item{rank, set * a.set_heads + (int)item - rank * a.set_heads};
+}
+
+// bytes up to the end of the last of `rows` rows, of `most` at most (no branches)
+template <int D>
+__device__ __forceinline__ unsigned bytes_of_rows(int rows, int most, unsigned row_bytes) {
+  return (unsigned)max(min(max(rows, 0), most) * (int)row_bytes - (int)(row_bytes - 2u * D), 0);
+}
+
+// Query rows q0 .. q0 + 31 of a prompt of n the slow way, straight from memory: running maximum, and a value only where it is seen.  `qf`: the
+// second operand of the products; the rows come out as the accumulators of O^T have them.
+template <int D>
+__device__ __forceinline__ void rows_the_slow_way(const bf16x8 (&qf)[D / 16], const u16* k_rows, long long k_token, const u16* v_rows, long long v_token, int q0,
+                                                  int n, float sl2, int l32, int g, f32x16 (&o)[D / 32], float& l_row) {
+  constexpr int kNK = D / 16, kND = D / 32;
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY;
+  l_row = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
+  for (int kb = 0; kb < min(n, q0 + 32); kb += 32) {
+    f32x16 s = zero;
+    const u16* const kr = k_rows + (long long)min(kb + l32, n - 1) * k_token + 8 * g;
+#pragma unroll
+    for (int st = 0; st < kNK; ++st)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kr + 16 * st)), qf[st], s, 0, 0, 0);
+    const int lim = q0 + l32 - kb - 4 * g;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = (8 * (r >> 2) + (r & 3) <= lim) ? s[r] : -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    const float m_new = fmaxf(m_run, max_with_other_half(mx)), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run - m_use) * sl2), neg = -m_use * sl2;
+    m_run = m_new;
+    l_row *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < kND; ++dt) o[dt] *= alpha;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sl2, neg));
+      sum += s[r];
+    }
+    l_row += sum_with_other_half(sum);
+    // key by key; key 8 (r / 4) + 4 half + r % 4 is in register r of the lanes of that half
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = kb + 8 * (r >> 2) + 4 * half + (r & 3);
+        const float mine = s[r], others = __shfl_xor(mine, 32), p = g == half ? mine : others;
+        const u16* const vr = v_rows + (long long)min(key, n - 1) * v_token + 4 * g;
+        const bool seen = key <= q0 + l32;
+#pragma unroll
+        for (int dt = 0; dt < kND; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(vr + 32 * dt + 8 * j);
+            const float v[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[dt][4 * j + e] = seen ? __builtin_fmaf(p, v[e], o[dt][4 * j + e]) : o[dt][4 * j + e];
+          }
+      }
+  }
+}
+
 template <int D, int KS>
 __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerSimd)) prompt_kernel(const PromptArgs a) {
   using S = Shape<D, KS>;
@@ -101,12 +179,9 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   u16* const lds_k = reinterpret_cast<u16*>(lds_raw + ks * S::kGroupLds);      // [2][kTile]
   u16* const lds_v = lds_k + 2 * S::kTile;                                     // [2][kTile]
 
-  // Dies and KV heads are dealt out to each other: dies_per_set dies share the query heads of as few KV heads as that allows, whose K and V
-  // their L2 caches then hold, and take turns along the list of (tile, query head).
-  const int xcd = blockIdx.x % kXcds, set = xcd / a.dies_per_set;
-  const unsigned item = blockIdx.x / kXcds * (unsigned)a.dies_per_set + (unsigned)(xcd - set * a.dies_per_set);
-  const int rank = (int)quotient(item, a.by_set_heads), h = set * a.set_heads + (int)item - rank * a.set_heads;
-  const PromptTile pt = find_tile(a, rank, lane);
+  const Item item = item_of(a);
+  const int rank = item.rank, h = item.head;
+  const PromptTile pt = find_tile<kPromptRows>(a, rank, lane);
   const int n = pt.length, wg_row = pt.tile * kPromptRows;
   if (wg_row >= n) return;
   const int hk = (int)quotient((unsigned)h, a.by_group);
@@ -144,9 +219,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
     unsigned bytes, row_bytes;
     int rows;                          // from this tile's first one on
   };
-  auto bytes_of = [&](int rows, unsigned row_bytes) __attribute__((always_inline)) -> unsigned {      // up to the end of the last row (no branches)
-    return (unsigned)max(min(max(rows, 0), kTileKeys) * (int)row_bytes - (int)(row_bytes - 2u * D), 0);
-  };
+  auto bytes_of = [&](int rows, unsigned row_bytes) __attribute__((always_inline)) -> unsigned { return bytes_of_rows<D>(rows, kTileKeys, row_bytes); };
   auto feed_at = [&](const u16* first, unsigned row_bytes, int rows) __attribute__((always_inline)) -> Feed {
     return Feed{(unsigned long long)first, bytes_of(rows, row_bytes), row_bytes, rows};
   };
@@ -442,57 +515,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   check[0] += check[1] + check[2] + check[3];
   check[4] += check[5] + check[6] + check[7];
   if (__any(!(l_row <= 0x1p64f) || !(check[0] + check[4] == 0.f))) {
-    // ---- the slow way: running maximum, one block of 32 keys at a time straight from memory
-    float m_run = -INFINITY;
-    l_row = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
-    for (int kb = 0; kb < min(n, q0 + 32); kb += 32) {
-      f32x16 s = zero;
-      const u16* const kr = k_rows + (long long)min(kb + l32, n - 1) * a.k_token + 8 * g;
-#pragma unroll
-      for (int st = 0; st < kNK; ++st)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kr + 16 * st)), qf[st], s, 0, 0, 0);
-      const int lim = q0 + l32 - kb - 4 * g;
-      float mx = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = (8 * (r >> 2) + (r & 3) <= lim) ? s[r] : -INFINITY;
-        mx = fmaxf(mx, s[r]);
-      }
-      const float m_new = fmaxf(m_run, max_with_other_half(mx)), m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run - m_use) * sl2), neg = -m_use * sl2;
-      m_run = m_new;
-      l_row *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < kND; ++dt) o[dt] *= alpha;
-      float sum = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sl2, neg));
-        sum += s[r];
-      }
-      l_row += sum_with_other_half(sum);
-      // key by key; key 8 (r / 4) + 4 half + r % 4 is in register r of the lanes of that half
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = kb + 8 * (r >> 2) + 4 * half + (r & 3);
-          const float mine = s[r], others = __shfl_xor(mine, 32), p = g == half ? mine : others;
-          const u16* const vr = v_rows + (long long)min(key, n - 1) * a.v_token + 4 * g;
-          const bool seen = key <= q0 + l32;
-#pragma unroll
-          for (int dt = 0; dt < kND; ++dt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const u32x2 w = *reinterpret_cast<const u32x2*>(vr + 32 * dt + 8 * j);
-              const float v[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[dt][4 * j + e] = seen ? __builtin_fmaf(p, v[e], o[dt][4 * j + e]) : o[dt][4 * j + e];
-            }
-        }
-    }
+    rows_the_slow_way<D>(qf, k_rows, a.k_token, v_rows, a.v_token, q0, n, sl2, l32, g, o, l_row);
   }
 
   // ---- rows to memory, through this wave's strip of LDS so that the stores are whole rows
@@ -515,35 +538,265 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   }
 }
 
-}  // namespace
+// ---- Few rows: workgroups of 128 would leave most of the chip idle and each have a long way to go.  Here one has 32 rows of one head, and its eight waves
+// share the keys, every eighth block of 32 each, as they come through two strips of LDS of the wave's own: no barrier between the query rows and
+// the end, where the waves' results are added up.  Bound by latency: the loads, a block or a few, and the sum over the waves.
+template <int D>
+struct FewShape {
+  static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32;
+  static constexpr int kChunks = D / 8, kRowsPerLoad = 64 / kChunks;
+  static constexpr int kLoads = 16 / kRowsPerLoad;             // for 16 rows
+  static constexpr int kStrip = 32 * D;                        // numbers: 32 keys
+  static constexpr int kWaveBytes = 2 * kStrip * 2;            // K, V; then what the wave leaves of its rows, as it is in the accumulators
+  static constexpr int kQ = kWaves * kWaveBytes, kStat = kQ + kRows * D * 2;
+  static constexpr int kLds = kStat + kWaves * 2 * kRows * 4;
+  static_assert(kRows * D * 4 <= kWaveBytes && kLds <= 160 * 1024, "LDS of a CU");
+};
 
-namespace {
+template <int D>
+__global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(const PromptArgs a) {
+  using S = FewShape<D>;
+  constexpr int kNK = D / 16, kNV = (D / 32) * 2, kND = D / 32;
+  extern __shared__ __align__(16) unsigned char lds_raw[];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Item item = item_of(a);
+  const PromptTile pt = find_tile<S::kRows>(a, item.rank, lane);
+  const int n = pt.length, q0 = pt.tile * S::kRows, h = item.head;
+  if (q0 >= n) return;
+  const int hk = (int)quotient((unsigned)h, a.by_group);
+  const u16* const q_rows = a.q + pt.begin * a.q_token + h * a.q_head;
+  const u16* const k_rows = a.k + pt.begin * a.k_token + hk * a.k_head;
+  const u16* const v_rows = a.v + pt.begin * a.v_token + hk * a.v_head;
+  u16* const out_rows = a.out + pt.begin * a.out_token + h * a.out_head;
+  const int rows_end = min(n, q0 + S::kRows), n_blocks = q0 / 32 + 1;         // blocks of keys; the last one has the diagonal
+  const float sl2 = a.scale_log2;
+
+  u16* const k_strip = reinterpret_cast<u16*>(lds_raw + wave * S::kWaveBytes);
+  u16* const v_strip = k_strip + S::kStrip;
+  u16* const q_lds = reinterpret_cast<u16*>(lds_raw + S::kQ);
+  float* const stats = reinterpret_cast<float*>(lds_raw + S::kStat);          // [wave][maxima, sums][row]
+  const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) void*)lds_raw);
+  const unsigned my_lds = lds_at + (unsigned)(wave * S::kWaveBytes);
+
+  // ---- global -> LDS, 16 rows at a time, through descriptors that end with the last row that is seen (as above; also why inline assembly)
+  const int ld_sub = lane / S::kChunks, ld_pos = lane % S::kChunks;
+  unsigned k_lane[S::kLoads], v_lane[S::kLoads];
+#pragma unroll
+  for (int j = 0; j < S::kLoads; ++j) {
+    const int row = S::kRowsPerLoad * j + ld_sub;
+    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks)) - 1024u * j;
+    v_lane[j] = (unsigned)row * a.v_bytes + 16u * (unsigned)(ld_pos ^ v_swizzle<D>(row)) - 1024u * j;
+  }
+  auto load16 = [&](const u16* first, int rows, unsigned row_bytes, const unsigned (&of)[S::kLoads], unsigned to) __attribute__((always_inline)) {
+    const unsigned long long at = (unsigned long long)first;
+    // (through the first lane: the compiler would carry some of it in vector registers)
+    const u32x4 buffer = {(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xFFFFu,
+                          (unsigned)__builtin_amdgcn_readfirstlane((int)bytes_of_rows<D>(rows, 16, row_bytes)), 0x00020000u};
+    if constexpr (S::kLoads == 4)
+      asm volatile("s_mov_b32 m0, %5\n\ts_nop 3\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
+                   "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds" ::"v"(of[0]), "v"(of[1]), "v"(of[2]), "v"(of[3]), "s"(buffer), "s"(to)
+                   : "m0", "memory");
+    else
+      asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\t"
+                   "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds" ::"v"(of[0]), "v"(of[1]), "s"(buffer), "s"(to)
+                   : "m0", "memory");
+  };
+  auto issue_k = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      load16(k_rows + (long long)(32 * b + 16 * i) * a.k_token, rows_end - 32 * b - 16 * i, a.k_bytes, k_lane, my_lds + 2u * (unsigned)(16 * i * D));
+  };
+  auto issue_v = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      load16(v_rows + (long long)(32 * b + 16 * i) * a.v_token, rows_end - 32 * b - 16 * i, a.v_bytes, v_lane, my_lds + 2u * (unsigned)(S::kStrip + 16 * i * D));
+  };
+  auto wait_all_but = [&](auto newest) __attribute__((always_inline)) {
+    constexpr int k = decltype(newest)::value;
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (k & 15) | (k >> 4 << 14));
+    asm volatile("" ::: "memory");
+  };
+  typedef std::integral_constant<int, 2 * S::kLoads> OneStrip;
+  typedef std::integral_constant<int, 4 * S::kLoads> BothStrips;
+  typedef std::integral_constant<int, 0> None;
+
+  // the query rows: a load of each wave (of the first four at d 64), for all; the wave's first block behind it
+  if (wave < 32 / S::kRowsPerLoad) {
+    const int row0 = S::kRowsPerLoad * wave, row = row0 + ld_sub;
+    const unsigned long long at = (unsigned long long)(q_rows + (long long)(q0 + row0) * a.q_token);
+    const u32x4 buffer = {(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xFFFFu,
+                          (unsigned)__builtin_amdgcn_readfirstlane((int)bytes_of_rows<D>(n - q0 - row0, S::kRowsPerLoad, a.q_bytes)), 0x00020000u};
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"((unsigned)ld_sub * a.q_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks))),
+                 "s"(buffer), "s"(lds_at + (unsigned)(S::kQ + 1024 * wave))
+                 : "m0", "memory");
+  }
+  if (wave < n_blocks) {
+    issue_k(wave);
+    issue_v(wave);
+    wait_all_but(BothStrips{});
+  } else {
+    wait_all_but(None{});
+  }
+  int k_off[kNK], v_off[kND];
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ (l32 % S::kChunks)));
+  {
+    const int rsub = 4 * g + ((lane & 15) >> 2), z = v_swizzle<D>(rsub);
+#pragma unroll
+    for (int dt = 0; dt < kND; ++dt) v_off[dt] = rsub * D + 8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ z) + 4 * (lane & 1);
+  }
+  __syncthreads();
+  bf16x8 qf[kNK];
+#pragma unroll
+  for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(q_lds + k_off[st]);
+
+  f32x16 o[kND];
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
+  float m = -INFINITY, l = 0.f;
+  for (int b = wave; b < n_blocks; b += S::kWaves) {
+    const bool more = b + S::kWaves < n_blocks;
+    wait_all_but(OneStrip{});
+    f32x16 s = zero;
+#pragma unroll
+    for (int st = 0; st < kNK; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_b128(k_strip + k_off[st]), qf[st], s, 0, 0, 0);
+    // K has been read; and a vector instruction may read a product 12 wait states after it, which the compiler does not see to in
+    // another basic block
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_nop 7" : "+v"(s)::"memory");
+    if (more) issue_k(b + S::kWaves);
+    if (b == n_blocks - 1) {                   // key 8 (r / 4) + 4 g + r % 4 of the block and row l32 of the tile
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) <= l32 - 4 * g ? s[r] : -INFINITY;
+    }
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = max_with_other_half(top);
+    if (__any(top > m)) {                       // a larger logit: what has been added up is brought onto it
+      const float m_new = fmaxf(m, top), by = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * sl2);
+      m = m_new;
+      l *= by;
+#pragma unroll
+      for (int dt = 0; dt < kND; ++dt) o[dt] *= by;
+    }
+    const float minus = m == -INFINITY ? 0.f : -m * sl2;
+    unsigned p[8];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sl2, minus)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], sl2, minus));
+      l += p0 + p1;
+      p[r / 2] = pack_bf16(p0, p1);
+    }
+    if (more) wait_all_but(OneStrip{});
+    else wait_all_but(None{});
+#pragma unroll
+    for (int vi = 0; vi < kNV; ++vi) {
+      const u32x4 pw = {p[4 * (vi % 2)], p[4 * (vi % 2) + 1], p[4 * (vi % 2) + 2], p[4 * (vi % 2) + 3]};
+      o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_vt(v_strip + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D), __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) issue_v(b + S::kWaves);
+  }
+
+  // ---- the waves' results, added up: a thread has eight channels of a row
+  if constexpr (kND == 4) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]));
+  else asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]));
+  if (wave < n_blocks) {
+    l = sum_with_other_half(l);
+    if (g == 0) {
+      stats[64 * wave + l32] = m;
+      stats[64 * wave + 32 + l32] = l;
+    }
+    f32x4* const left = reinterpret_cast<f32x4*>(k_strip) + lane;
+#pragma unroll
+    for (int k = 0; k < 4 * kND; ++k) left[64 * k] = f32x4{o[k / 4][4 * (k % 4)], o[k / 4][4 * (k % 4) + 1], o[k / 4][4 * (k % 4) + 2], o[k / 4][4 * (k % 4) + 3]};
+  }
+  __syncthreads();
+  const int row = tid % 32, chunk = tid / 32, in_use = min(n_blocks, S::kWaves);
+  if (chunk >= S::kChunks) return;
+  float top = stats[row];
+  for (int w = 1; w < in_use; ++w) top = fmaxf(top, stats[64 * w + row]);
+  const float use = top == -INFINITY ? 0.f : top;
+  float l_row = 0.f;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  for (int w = 0; w < in_use; ++w) {
+    const float f = __builtin_amdgcn_exp2f((stats[64 * w + row] - use) * sl2);
+    const f32x4* const left = reinterpret_cast<const f32x4*>(lds_raw + w * S::kWaveBytes) + 64 * chunk + row;
+    l_row += f * stats[64 * w + 32 + row];
+    lo += f * left[0];
+    hi += f * left[32];
+  }
+  // what is not finite is not 0 when it is multiplied by 0: a value that the row does not see may be in it
+  const float check = ((lo[0] + lo[1]) + (lo[2] + lo[3]) + ((hi[0] + hi[1]) + (hi[2] + hi[3]))) * 0.f + l_row * 0.f;
+  if (__any(!(check == 0.f))) {
+    rows_the_slow_way<D>(qf, k_rows, a.k_token, v_rows, a.v_token, q0, n, sl2, l32, g, o, l_row);
+    const float inv = 1.f / l_row;
+#pragma unroll
+    for (int k = 0; k < 4 * kND; ++k)           // this wave's chunks
+      if (k / 2 == wave && q0 + l32 < n)
+        *reinterpret_cast<u32x2*>(out_rows + (long long)(q0 + l32) * a.out_token + 8 * k + 4 * g) =
+            u32x2{pack_bf16(o[k / 4][4 * (k % 4)] * inv, o[k / 4][4 * (k % 4) + 1] * inv), pack_bf16(o[k / 4][4 * (k % 4) + 2] * inv, o[k / 4][4 * (k % 4) + 3] * inv)};
+    return;
+  }
+  const float inv = 1.f / l_row;
+  if (q0 + row < n)
+    *reinterpret_cast<u32x4*>(out_rows + (long long)(q0 + row) * a.out_token + 8 * chunk) =
+        u32x4{pack_bf16(lo[0] * inv, lo[1] * inv), pack_bf16(lo[2] * inv, lo[3] * inv), pack_bf16(hi[0] * inv, hi[1] * inv), pack_bf16(hi[2] * inv, hi[3] * inv)};
+}
+
 template <int D, int KS>
 hipError_t prepare() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<D, KS>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<D, KS>::kLds);
 }
-template <int D, int KS>
-hipError_t launch(const PromptArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((prompt_kernel<D, KS>), dim3(a.workgroups), dim3(Shape<D, KS>::kThreads), (Shape<D, KS>::kLds), s, a);
-  return hipGetLastError();
+template <int D>
+hipError_t prepare_few() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_few_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kLds);
 }
-}  // namespace
 
-hipError_t prepare_prompt() {
-  hipError_t e;
-  if ((e = prepare<128, 1>()) != hipSuccess || (e = prepare<128, 2>()) != hipSuccess || (e = prepare<64, 1>()) != hipSuccess) return e;
-  return prepare<64, 2>();
+// The grid for tiles of so many rows: every prompt may have one that is not full.
+unsigned deal_out(PromptArgs& a, int rows) {
+  const long long tiles = ((long long)a.n_tokens + (long long)(rows - 1) * a.n_seqs) / rows;
+  const unsigned items = (unsigned)(tiles * a.set_heads), per_die = (items + a.dies_per_set - 1) / a.dies_per_set;
+  a.by_set_heads = divisor_of((unsigned)a.set_heads, items + kXcds);
+  return kXcds * per_die;
 }
 
 // Two groups of waves share the keys where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of the
 // time), or nearly so and the longest of them decides, and the prompts are not too short for it.  One prompt of 32/8 heads, one group and two: d 128, 128 rows
 // 6.5 and 7.6 us, 256 8.6 and 8.9, 512 12.3 and 11.9, 1536 30.3 and 27.4, 4096 132 and 136, 8000 rows of 8/2 heads (504 workgroups) 138 and 122, 16000 of 4/4 (500)
 // 270 and 233; d 64, 256 rows 6.8 and 6.6, 512 9.4 and 8.5, 1024 15.2 and 12.6, 16000 of 4/4 170 and 150.  8 prompts of 500 rows, 16/4 heads, d 128, 18.0 and 23.7.
-hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) {
+constexpr unsigned kFewWorkgroups = 512;
+template <int D>
+hipError_t launch(PromptArgs a, hipStream_t s) {
   const long long mean = a.n_tokens / a.n_seqs;
-  const bool few = (a.workgroups <= 256 && mean >= 384) || (a.workgroups <= 512 && mean >= 1024);
-  if (head_dim == 128) return few ? launch<128, 2>(a, s) : launch<128, 1>(a, s);
-  return few ? launch<64, 2>(a, s) : launch<64, 1>(a, s);
+  unsigned grid = deal_out(a, FewShape<D>::kRows);
+  if (grid <= kFewWorkgroups) {
+    hipLaunchKernelGGL(prompt_few_kernel<D>, dim3(grid), dim3(FewShape<D>::kThreads), FewShape<D>::kLds, s, a);
+    return hipGetLastError();
+  }
+  grid = deal_out(a, kPromptRows);
+  if ((grid <= 256 && mean >= 384) || (grid <= 512 && mean >= 1024))
+    hipLaunchKernelGGL((prompt_kernel<D, 2>), dim3(grid), dim3(Shape<D, 2>::kThreads), (Shape<D, 2>::kLds), s, a);
+  else
+    hipLaunchKernelGGL((prompt_kernel<D, 1>), dim3(grid), dim3(Shape<D, 1>::kThreads), (Shape<D, 1>::kLds), s, a);
+  return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t prepare_prompt() {
+  hipError_t e;
+  if ((e = prepare<128, 1>()) != hipSuccess || (e = prepare<128, 2>()) != hipSuccess || (e = prepare<64, 1>()) != hipSuccess) return e;
+  if ((e = prepare<64, 2>()) != hipSuccess || (e = prepare_few<64>()) != hipSuccess) return e;
+  return prepare_few<128>();
+}
+
+hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) { return head_dim == 128 ? launch<128>(a, s) : launch<64>(a, s); }
 
 }  // namespace kvp

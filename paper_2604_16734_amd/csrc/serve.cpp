@@ -147,9 +147,7 @@ int kvp_prompt_attention(const kvp_prompts* p, void* stream) {
   for (const auto& s : strides)
     if (!valid_strides(s[0], s[1]) || (p->n_tokens > 1 && s[0] < p->head_dim)) return KVP_EINVAL;
   if (!separate_rows(p->out_token, p->out_head, p->n_tokens, p->n_q_heads, p->head_dim)) return KVP_EINVAL;
-  // tiles of rows, at most: every prompt may have one that is not full
-  const long long tiles = ((long long)p->n_tokens + (long long)(kPromptRows - 1) * p->n_seqs) / kPromptRows;
-  if (tiles * p->n_q_heads > (1ll << 30) - 64) return KVP_EINVAL;
+  if (((long long)p->n_tokens / 32 + p->n_seqs) * p->n_q_heads > (1ll << 30) - 64) return KVP_EINVAL;
   if (p->n_tokens == 0) return KVP_OK;
   if (!aligned(p->q, 16) || !aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->out, 16)) return KVP_EINVAL;
   if (const int rc = prepared()) return rc;
@@ -171,9 +169,6 @@ int kvp_prompt_attention(const kvp_prompts* p, void* stream) {
   while (p->n_kv_heads % sets != 0) sets /= 2;
   a.dies_per_set = kXcds / sets;
   a.set_heads = p->n_q_heads / sets;
-  const unsigned items = (unsigned)(tiles * a.set_heads), per_die = (items + a.dies_per_set - 1) / a.dies_per_set;
-  a.workgroups = kXcds * per_die;
-  a.by_set_heads = divisor_of((unsigned)a.set_heads, items + kXcds);
   a.by_group = divisor_of((unsigned)(p->n_q_heads / p->n_kv_heads), (unsigned)p->n_q_heads);
   a.scale_log2 = scale_log2_of(p->softmax_scale, p->head_dim);
   return code_of(launch_prompt(a, p->head_dim, static_cast<hipStream_t>(stream)));

@@ -46,7 +46,7 @@ hipError_t prepare_paged_decode();      // function attributes on the current de
 int paged_decode_workgroups(int head_dim, bool e4m3);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int head_dim, bool e4m3, hipStream_t s);
 
-constexpr int kPromptRows = 128;       // query rows of a workgroup
+constexpr int kPromptRows = 128;       // query rows of a workgroup, where there are many
 struct PromptArgs {
   const u16* q;
   const u16* k;
@@ -57,7 +57,6 @@ struct PromptArgs {
   unsigned q_bytes, k_bytes, v_bytes;      // from token to token
   int n_tokens, n_seqs, n_q_heads;
   int dies_per_set, set_heads;             // dies that share set_heads query heads
-  unsigned workgroups;
   Divisor by_set_heads, by_group;
   float scale_log2;
 };
