@@ -550,6 +550,7 @@ struct FewShape {
   static constexpr int kWaveBytes = 2 * kStrip * 2;            // K, V; then what the wave leaves of its rows, as it is in the accumulators
   static constexpr int kQ = kWaves * kWaveBytes, kStat = kQ + kRows * D * 2;
   static constexpr int kLds = kStat + kWaves * 2 * kRows * 4;
+  static constexpr unsigned kPerCu = kLds > 80 * 1024 ? 1 : 2;
   static_assert(kRows * D * 4 <= kWaveBytes && kLds <= 160 * 1024, "LDS of a CU");
 };
 
@@ -767,16 +768,19 @@ unsigned deal_out(PromptArgs& a, int rows) {
   return kXcds * per_die;
 }
 
-// Two groups of waves share the keys where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of the
-// time), or nearly so and the longest of them decides, and the prompts are not too short for it.  One prompt of 32/8 heads, one group and two: d 128, 128 rows
-// 6.5 and 7.6 us, 256 8.6 and 8.9, 512 12.3 and 11.9, 1536 30.3 and 27.4, 4096 132 and 136, 8000 rows of 8/2 heads (504 workgroups) 138 and 122, 16000 of 4/4 (500)
-// 270 and 233; d 64, 256 rows 6.8 and 6.6, 512 9.4 and 8.5, 1024 15.2 and 12.6, 16000 of 4/4 170 and 150.  8 prompts of 500 rows, 16/4 heads, d 128, 18.0 and 23.7.
-constexpr unsigned kFewWorkgroups = 512;
+// Three ways, by the workgroups that there would be and the mean length of the prompts.
+// 32 rows: while the chip holds all of these workgroups at once, one per CU at d 128 and two at 64, or twice as many of long prompts.  Against 128 rows,
+// d 128: 4 heads of 608 rows (76 workgroups) 8.3 and 11.6 us, 32 of 256 (256) 6.8 and 8.5, 32 of 384 (384) 10.7 and 10.4, 16 of 1024 (512) 15.9 and 16.1, 8 of
+// 2000 (504) 21.3 and 24.2, 8 of eight prompts of 200 (448) 10.6 and 8.3; d 64: 32 of 512 (512) 7.5 and 8.2, 32 of 640 (640) 10.5 and 9.3.
+// 128 rows and two groups of waves that share the keys: where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of
+// the time), or nearly so and the longest of them decides, and the prompts are not too short for it.  One group and two, d 128: 32 heads of 512 rows
+// 12.3 and 11.9 us, 1536 30.3 and 27.4, 4096 132 and 136, 8 of 8000 (504 workgroups) 138 and 122, 4 of 16000 (500) 270 and 233, 16 of eight prompts of 500
+// (512) 18.0 and 23.7; d 64, 4 of 16000 170 and 150.
 template <int D>
 hipError_t launch(PromptArgs a, hipStream_t s) {
   const long long mean = a.n_tokens / a.n_seqs;
   unsigned grid = deal_out(a, FewShape<D>::kRows);
-  if (grid <= kFewWorkgroups) {
+  if (grid <= 256 * FewShape<D>::kPerCu || (grid <= 512 && mean >= 1024)) {
     hipLaunchKernelGGL(prompt_few_kernel<D>, dim3(grid), dim3(FewShape<D>::kThreads), FewShape<D>::kLds, s, a);
     return hipGetLastError();
   }
