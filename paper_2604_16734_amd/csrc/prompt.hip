@@ -33,6 +33,11 @@ constexpr int kWaves = 4;              // of a workgroup, or of each half of one
 static_assert(kPromptRows == 32 * kWaves, "rows of a workgroup");
 constexpr int kTileKeys = 64;
 
+// In LDS the 16-byte chunk ch of a row of K (or of Q, or of the result) lies at position ch ^ k_swizzle(row): sixteen rows, read in the same column, are
+// then in all of the 64 banks.  (At d 64 two rows fill them.  With the row's number itself a third of all LDS cycles were conflicts, now 3 %; the time is the same, as LDS is not what it waits for.)
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row) { return D == 64 ? row / 2 % 8 : row % 16; }
+
 // KS: groups of four waves that share the keys of the same rows, tile by tile in turns
 template <int D, int KS>
 struct Shape {
@@ -211,7 +216,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
 #pragma unroll
   for (int j = 0; j < S::kLoads; ++j) {
     const int row = 16 * wave + S::kRowsPerLoad * j + ld_sub;
-    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks)) - 1024u * j;
+    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row)) - 1024u * j;
     v_lane[j] = (unsigned)row * a.v_bytes + 16u * (unsigned)(ld_pos ^ v_swizzle<D>(row)) - 1024u * j;
   }
   struct Feed {
@@ -251,7 +256,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   // ---- where the fragments are (in numbers)
   int k_off[kNK], v_off[kND];
 #pragma unroll
-  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ (l32 % S::kChunks)));
+  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ k_swizzle<D>(l32)));
   {
     const int rsub = 4 * g + ((lane & 15) >> 2), z = v_swizzle<D>(rsub);
 #pragma unroll
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
 #pragma unroll
     for (int j = 0; j < 2 * S::kLoads; ++j) {
       const int row = S::kRowsPerLoad * j + ld_sub;
-      const unsigned of = (unsigned)row * a.q_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks));
+      const unsigned of = (unsigned)row * a.q_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row));
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of), "s"(buffer), "s"(to + 1024u * j) : "m0", "memory");
     }
   }
@@ -528,12 +533,12 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
       const f32x16& x = o[dt];
       const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j] * inv, x[4 * j + 1] * inv), pack_bf16(x[4 * j + 4] * inv, x[4 * j + 5] * inv), false, false);
       const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j + 2] * inv, x[4 * j + 3] * inv), pack_bf16(x[4 * j + 6] * inv, x[4 * j + 7] * inv), false, false);
-      rows[l32 * S::kChunks + ((4 * dt + j + g) ^ (l32 % S::kChunks))] = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      rows[l32 * S::kChunks + ((4 * dt + j + g) ^ k_swizzle<D>(l32))] = u32x4{lo[0], hi[0], lo[1], hi[1]};
     }
 #pragma unroll
   for (int it = 0; it < S::kChunks / 2; ++it) {
     const int r = (64 * it + lane) / S::kChunks, ch = lane % S::kChunks;
-    const u32x4 val = rows[r * S::kChunks + (ch ^ (r % S::kChunks))];
+    const u32x4 val = rows[r * S::kChunks + (ch ^ k_swizzle<D>(r))];
     if (q0 + r < n) *reinterpret_cast<u32x4*>(out_rows + (long long)(q0 + r) * a.out_token + 8 * ch) = val;
   }
 }
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
 #pragma unroll
   for (int j = 0; j < S::kLoads; ++j) {
     const int row = S::kRowsPerLoad * j + ld_sub;
-    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks)) - 1024u * j;
+    k_lane[j] = (unsigned)row * a.k_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row)) - 1024u * j;
     v_lane[j] = (unsigned)row * a.v_bytes + 16u * (unsigned)(ld_pos ^ v_swizzle<D>(row)) - 1024u * j;
   }
   auto load16 = [&](const u16* first, int rows, unsigned row_bytes, const unsigned (&of)[S::kLoads], unsigned to) __attribute__((always_inline)) {
@@ -632,7 +637,7 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
     const unsigned long long at = (unsigned long long)(q_rows + (long long)(q0 + row0) * a.q_token);
     const u32x4 buffer = {(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xFFFFu,
                           (unsigned)__builtin_amdgcn_readfirstlane((int)bytes_of_rows<D>(n - q0 - row0, S::kRowsPerLoad, a.q_bytes)), 0x00020000u};
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"((unsigned)ld_sub * a.q_bytes + 16u * (unsigned)(ld_pos ^ (row % S::kChunks))),
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"((unsigned)ld_sub * a.q_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row))),
                  "s"(buffer), "s"(lds_at + (unsigned)(S::kQ + 1024 * wave))
                  : "m0", "memory");
   }
@@ -645,7 +650,7 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
   }
   int k_off[kNK], v_off[kND];
 #pragma unroll
-  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ (l32 % S::kChunks)));
+  for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ k_swizzle<D>(l32)));
   {
     const int rsub = 4 * g + ((lane & 15) >> 2), z = v_swizzle<D>(rsub);
 #pragma unroll
