@@ -18,9 +18,9 @@
 //   phase 2   MFMA: S_X(t+1), O += P_X(t) V     | vector: P_Y(t) = exp(S_Y(t) - m), the loads of K(t+2) and V(t+1)
 //
 // Softmax reference.  exp(S - m) is exact for any m as long as nothing overflows: a row takes the maximum of the first 32 keys that it
-// sees and O is never rescaled.  A row sum beyond 2^64 says that this did not do; a result that is not finite may also come from a value that the
-// row does not see, because 0 times infinity is no 0.  In both cases the wave takes its rows again the slow way, with a running maximum and
-// values only where they are seen.
+// sees and O is never rescaled.  A row sum beyond 2^64 says that this did not do, and minus infinity is no reference; a result that is not finite may also
+// come from a value that the row does not see, because 0 times infinity is no 0.  In these cases the wave takes its rows again the slow way, with a
+// running maximum and values only where they are seen.
 #include <type_traits>
 
 #include "mfma_tools.h"
@@ -485,6 +485,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   if constexpr (kND == 4) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]));       // (as after the first products)
   else asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]));
   float l_row = sum_with_other_half(l_run);
+  if (m_ref == -INFINITY && q0 + l32 >= kTileKeys * ks) l_row = NAN;           // keys, but no reference
   if constexpr (KS == 2) {
     // the second group leaves its rows as they lie in the accumulators, and the first one adds them up
     float* const stat = reinterpret_cast<float*>(lds_raw + S::kGroupLds + kPromptRows * D * 4) + 64 * wave;       // [row, or 32 + row]

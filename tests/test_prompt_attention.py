@@ -82,7 +82,7 @@ def test_long_prompts(hq, hkv, d, n):
 
 @gpu
 @pytest.mark.parametrize("how,other", [("rows", "heads"), ("heads", "projection"), ("projection", "rows")])
-@pytest.mark.parametrize("hq,hkv,d", [(6, 2, 128), (16, 8, 64)])
+@pytest.mark.parametrize("hq,hkv,d", [(6, 2, 128), (16, 8, 64), (84, 28, 128), (96, 6, 64)])
 def test_strides(hq, hkv, d, how, other):
     gen = torch.Generator().manual_seed(d)
     begin = [0, 70, 333]
@@ -113,13 +113,14 @@ def test_many_prompts():
     same(out, ref, size, most, 64)
 
 
+# few rows for the chip, many, and many of few heads
 @gpu
+@pytest.mark.parametrize("n,hq,hkv", [(450, 4, 2), (450, 96, 48), (900, 24, 12)])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("what", [float("inf"), float("nan"), -3e38])
-def test_what_a_row_does_not_see_has_no_part_in_it(d, what):
+def test_what_a_row_does_not_see_has_no_part_in_it(d, what, n, hq, hkv):
     """Keys and values that are not finite, or as small as their type has them: rows before them have the bits that they have without them."""
     gen = torch.Generator().manual_seed(d)
-    n, hq, hkv = 450, 4, 2
     q, k, v = (x.to(DEV) for x in (randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)))
     begin = int32([0, 100, n])
     good = K.prompt_attention(q, k, v, begin)
@@ -139,11 +140,12 @@ def test_what_a_row_does_not_see_has_no_part_in_it(d, what):
 
 
 @gpu
+@pytest.mark.parametrize("hq,hkv", [(2, 1), (96, 48), (48, 24)])
 @pytest.mark.parametrize("d", [64, 128])
-def test_logits_that_run_away(d):
+def test_logits_that_run_away(d, hq, hkv):
     """Logits far above those of the first keys, past what a fixed reference takes, in single rows and in all of them."""
     gen = torch.Generator().manual_seed(7)
-    n, hq, hkv = 400, 2, 1
+    n = 400
     for rows in (slice(250, 251), slice(40, n)):
         q, k, v = randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)
         q[rows] = (30 * q[rows].float()).to(torch.bfloat16)
@@ -153,6 +155,23 @@ def test_logits_that_run_away(d):
         torch.cuda.synchronize()
         ref, size, most = causal(q, k, v, [0, n], d ** -0.5)
         same(out, ref, size, most, d)
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv", [(2, 1), (96, 48), (48, 24)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [0.25, 20.0])
+def test_first_keys_that_weigh_nothing(d, hq, hkv, size):
+    """Logits of minus infinity before all others, which are about 0 or far below it."""
+    gen = torch.Generator().manual_seed(8)
+    n, first = 500, 40
+    q, k, v = randn(gen, n, hq, d).abs() + 0.125, -size * (1 + randn(gen, n, hkv, d).abs()), randn(gen, n, hkv, d)
+    k[:first] = -math.inf
+    out = K.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), int32([0, n]))
+    torch.cuda.synchronize()
+    ref, size, most = causal(q, k, v, [0, n], d ** -0.5)
+    assert np.isfinite(ref[first:]).all()
+    same(out, ref, size, most, d)
 
 
 @gpu
@@ -170,9 +189,10 @@ def test_bounds_out_of_range():
 
 
 @gpu
-def test_prompts_on_another_stream_and_in_a_graph():
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (96, 24, 64), (96, 8, 128)])
+def test_prompts_on_another_stream_and_in_a_graph(hq, hkv, d):
     gen = torch.Generator().manual_seed(6)
-    n, hq, hkv, d = 500, 8, 2, 128
+    n = 500
     q, k, v = (x.to(DEV) for x in (randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)))
     begin, out = int32([0, 100, 500]), torch.zeros_like(q)
     side = torch.cuda.Stream()
