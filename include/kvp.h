@@ -428,8 +428,8 @@ typedef struct kvp_rows {
  *   first      device [n_seqs], or NULL
  * A token is left out that has no sequence (before seq_begin[0], or from
  * seq_begin[n_seqs] on), whose place lies outside the table, or whose page number is
- * not in 0 .. n_pages - 1.  Of tokens with the same place in the pages each number is
- * left by one of them.  Nothing else in the pages is touched.  n_tokens = 0 does nothing. */
+ * not in 0 .. n_pages - 1.  Of tokens with the same place in the pages each number and
+ * exponent is left by one of them, not all by the same one.  Nothing else in the pages is touched.  n_tokens = 0 does nothing. */
 int kvp_page_write(const kvp_pages* pages, const kvp_rows* rows, const int32_t* seq_begin, const int32_t* table,
                    int32_t table_width, const int32_t* first, int32_t n_seqs, void* stream);
 

@@ -82,7 +82,7 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
       }
       // of the sequences that have a tile lo, the one before which so many come
       unsigned long long there = __ballot(tiles > lo);
-      for (int skip = rank - from_hi; skip > 0; --skip) there &= there - 1;
+      for (int skip = min(rank - from_hi, 63); skip > 0; --skip) there &= there - 1;        // (below 64 if the bounds do not descend)
       const int i = __builtin_ctzll(there);
       return PromptTile{__builtin_amdgcn_readlane(begin, i), __builtin_amdgcn_readlane(end - begin, i), lo};
     }

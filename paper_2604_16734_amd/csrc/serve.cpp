@@ -36,7 +36,7 @@ bool valid_strides(int64_t token, int64_t head) {
 bool separate_rows(int64_t token, int64_t head, int n_tokens, int n_heads, int dim) {
   if ((n_tokens > 1 && token < dim) || (n_heads > 1 && head < dim)) return false;
   if (n_tokens <= 1 || n_heads <= 1) return true;
-  return token >= (n_heads - 1) * head + dim || head >= (n_tokens - 1) * token + dim;
+  return token >= (__int128)(n_heads - 1) * head + dim || head >= (n_tokens - 1) * token + dim;       // (heads times their distance may pass 64 bits)
 }
 
 bool valid_table(const int32_t* table, int32_t width, int32_t page_size, int32_t n_seqs) {
