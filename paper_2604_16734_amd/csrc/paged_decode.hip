@@ -72,11 +72,18 @@ __device__ __forceinline__ bf16x8 eight_of_e4m3(unsigned lo, unsigned hi, float 
   return __builtin_bit_cast(bf16x8, w);
 }
 // the larger one, in one instruction (fmaxf makes NaNs quiet first, with one more for each operand)
-__device__ __forceinline__ float max_of(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
-// 2^e of the i-th of four exponents
-__device__ __forceinline__ float power_of(unsigned exps, int i) {
-  return __uint_as_float((i < 3 ? exps << (23 - 8 * i) : exps >> 1) & 0x7F800000u);
+__device__ __forceinline__ float max_of(float x, float y) {
+  float m;
+  asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(x), "v"(y));
+  return m;
 }
+__device__ __forceinline__ float max_of(float x, float y, float z) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(x), "v"(y), "v"(z));
+  return m;
+}
+// 2^e of the i-th of four exponents
+__device__ __forceinline__ float power_of(unsigned exps, int i) { return __uint_as_float((exps >> (8 * i) & 0xFFu) << 23); }
 // two transposing reads: four keys of this lane's channel, and the four that lie `rows` bytes further
 __device__ __forceinline__ bf16x8 lds_read_vt16(const unsigned char* p, int rows) {
   const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 __attribute__((address_space(3)))*)(p));
@@ -103,7 +110,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
 
   // ---- this workgroup's share, and the sequence that it begins in
   unsigned at = 0, end = 1, share = 1;
-  int seq = -1, n_keys = 0, direct_head = 0, ids = -1;
+  int seq = -1, n_keys = 0, direct_head = 0;
   // of 64 sequences at a time: lengths, and the units up to each
   int group0 = 0, length = 0;
   unsigned before = 0, tiles = 0, upto = 0;
@@ -114,10 +121,16 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     tiles = (unsigned)paged_tiles(length) * (unsigned)a.pool.n_heads;
     upto = (unsigned)sum_upto((int)tiles);
   };
+  // lane i: the page of block i % 2 of this wave's 32 keys in tile base + i / 2
+  int ids = -1;
+  auto load_ids = [&](int base, int most) __attribute__((always_inline)) {
+    const int at = kPagedTile * (base + lane / 2) + kKeys * wave + 16 * (lane & 1);
+    ids = at < most ? a.table[(size_t)seq * a.width + (at >> a.pool.shift)] : -1;
+  };
   if constexpr (kDirect) {
     seq = (int)quotient(blockIdx.x, a.by_heads);
     direct_head = (int)blockIdx.x - seq * a.pool.n_heads;
-    ids = lane < a.width ? a.table[(size_t)seq * a.width + lane] : -1;       // (beside the length, not after it)
+    load_ids(0, a.width << a.pool.shift);            // (beside the length, not after it)
     n_keys = __builtin_amdgcn_readfirstlane(length_of(a, seq));
     if (n_keys == 0) {
       for (int i = threadIdx.x; i < a.group * D / 8; i += kThreads)
@@ -172,11 +185,11 @@ paged_decode_kernel(const PagedDecodeArgs a) {
                    "buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(of[0]), "s"(buffer), "s"(to)
                    : "m0", "memory");
   };
-  auto buffer_at = [&](const char* base, int rows) __attribute__((always_inline)) -> u32x4 {
+  auto buffer_at = [&](const char* base, unsigned bytes) __attribute__((always_inline)) -> u32x4 {
     const unsigned long long x = (unsigned long long)base;
     // (through the first lane: the compiler would carry some of it in vector registers)
     return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((int)x), (unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) & 0xFFFFu,
-                 (unsigned)__builtin_amdgcn_readfirstlane(rows * kRow), 0x00020000u};
+                 (unsigned)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
   };
   auto wait_all_but = [&](auto newest) __attribute__((always_inline)) {
     constexpr int k = decltype(newest)::value;
@@ -221,23 +234,21 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     const int head = kDirect ? direct_head : __builtin_amdgcn_readfirstlane((int)((at - seq_first) / n_tiles));
     const unsigned first = seq_first + (unsigned)head * n_tiles;      // the first unit of this sequence and head
     const int t0 = kDirect ? 0 : (int)(at - first), t1 = kDirect ? (int)n_tiles : (int)(min(end, first + n_tiles) - first);
-    const int32_t* const row_of_table = a.table + (size_t)seq * a.width;
 
-    // where the rows of 64 columns from col0 on begin, for this head, in rows of the pages; negative: no such page
-    int col0 = 0;
-    long long page_rows = -1;
-    auto rows_of_ids = [&]() __attribute__((always_inline)) {
-      page_rows = ids < 0 || ids >= a.pool.n_pages ? -1ll : (long long)page_row(ids, a.pool.n_heads, head, 0, a.pool.shift);
-      asm volatile("" : "+v"(page_rows));               // here, not where it is used: the wait there would be for all loads, every time
+    // Where the two blocks of 16 keys of 32 tiles, from tile base on, begin in the pages, and how many bytes of them there are: one to a lane, as
+    // in ids.  (Read out of there, three numbers for a block, they cost a tile a third of what finding them costs.)
+    int base = t0;
+    unsigned long long block_at = 0;
+    unsigned block_bytes = 0;
+    auto find_blocks = [&]() __attribute__((always_inline)) {
+      const int at = kPagedTile * (base + lane / 2) + kKeys * wave + 16 * (lane & 1);
+      const bool there = at < n_keys && ids >= 0 && ids < a.pool.n_pages;
+      block_at = there ? page_row(ids, a.pool.n_heads, head, place_of(at, a.pool.shift).offset, a.pool.shift) * kRow : 0ull;
+      block_bytes = there ? (unsigned)min(16, n_keys - at) * kRow : 0u;
+      asm volatile("" : "+v"(block_at), "+v"(block_bytes));      // here, not where they are used: the wait there would be for all loads, every time
     };
-    auto load_ids = [&](int col) __attribute__((always_inline)) {
-      col0 = col;
-      ids = col + lane < a.width ? row_of_table[col + lane] : -1;
-      rows_of_ids();
-    };
-    const int kb0 = kPagedTile * t0 + kKeys * wave;
-    if (kDirect) rows_of_ids();
-    else if (kb0 < n_keys) load_ids(kb0 >> a.pool.shift);
+    if (kDirect) find_blocks();
+    else load_ids(base, n_keys);
 
     // Q: second operand, column l16 of the products; channels in the order of K's fragments
     bf16x8 qf[kSteps];
@@ -249,47 +260,49 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         qf[st] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + ch));
       }
     }
+    if (!kDirect) find_blocks();
     f32x4 o[kTiles];
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    // rows of the two blocks of a tile that take part, and where they are
     struct Tile {
-      int rows[2];
-      long long at[2];
+      unsigned long long at[2];          // its blocks in the pages
+      unsigned bytes[2];                 // of them that take part
     };
     const int my_end = min(t1, (n_keys - kKeys * wave + kPagedTile - 1) / kPagedTile);      // tiles in which this wave has keys
     auto tile_at = [&](int t) __attribute__((always_inline)) -> Tile {
-      const int kb = kPagedTile * t + kKeys * wave;
+      if (!kDirect && t - base >= 32) {
+        load_ids(t, n_keys);
+        base = t;
+        find_blocks();
+      }
       Tile x;
-      if (((kb + 16) >> a.pool.shift) - col0 >= 64) load_ids(kb >> a.pool.shift);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const PagePlace p = place_of(kb + 16 * b, a.pool.shift);
-        const int hi = __builtin_amdgcn_readlane((int)(page_rows >> 32), p.column - col0), none = hi >> 31;       // (no branches)
-        const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)page_rows, p.column - col0);
-        x.rows[b] = min(16, max(0, n_keys - kb - 16 * b)) & ~none;
-        x.at[b] = (long long)((unsigned long long)(unsigned)(hi & ~none) << 32 | (lo & ~(unsigned)none)) + p.offset;
+        const int i = 2 * (t - base) + b;
+        const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(block_at >> 32), i), lo = (unsigned)__builtin_amdgcn_readlane((int)block_at, i);
+        x.at[b] = (unsigned long long)hi << 32 | lo;
+        x.bytes[b] = (unsigned)__builtin_amdgcn_readlane((int)block_bytes, i);
       }
       return x;
     };
     auto issue_k = [&](const Tile& x) __attribute__((always_inline)) {
       const unsigned to = lds_at;
       if constexpr (kE4m3) {                      // four exponents a lane: of block lane / 4 % 2, K's and V's
-        const long long row = lane & 4 ? x.at[1] : x.at[0];
+        const unsigned long long at0 = x.at[0] / kRow, at1 = x.at[1] / kRow, row = lane & 4 ? at1 : at0;
         const uint8_t* const src = (lane & 8 ? a.pool.v_exp : a.pool.k_exp) + row + 4 * (lane & 3);
         asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(to + 2 * S::kStrip) : "m0", "memory");
       }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.k + x.at[b] * kRow, x.rows[b]), k_lane, to + b * 16 * kRow);
+      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.k + x.at[b], x.bytes[b]), k_lane, to + b * 16 * kRow);
     };
     auto issue_v = [&](const Tile& x) __attribute__((always_inline)) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.v + x.at[b] * kRow, x.rows[b]), v_lane[b], lds_at + S::kStrip + b * 16 * kRow);
+      for (int b = 0; b < 2; ++b) load_rows(buffer_at(a.pool.v + x.at[b], x.bytes[b]), v_lane[b], lds_at + S::kStrip + b * 16 * kRow);
     };
 
-    Tile next{{0, 0}, {0, 0}};
+    Tile next{{0ull, 0ull}, {0u, 0u}};
     if (t0 < my_end) {
       next = tile_at(t0);
       issue_k(next);
@@ -333,12 +346,15 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         issue_k(next);
       }
       // ---- weights
-      const bool masked = now.rows[0] + now.rows[1] < kKeys;
-      if (masked) {
+      if (now.bytes[0] + now.bytes[1] < kKeys * kRow) {         // no row: no weight, and no exponent
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 4 * g + i % 4 < now.rows[i / 4] ? s[i / 4][i % 4] : -INFINITY;
+        for (int i = 0; i < 8; ++i) {
+          const bool there = 4 * g + i % 4 < (int)(now.bytes[i / 4] / kRow);
+          s[i / 4][i % 4] = there ? s[i / 4][i % 4] : -INFINITY;
+          if constexpr (kE4m3) v_exp[i / 4] = there ? v_exp[i / 4] : v_exp[i / 4] & ~(0xFFu << (8 * (i % 4)));
+        }
       }
-      float top = max_of(max_of(max_of(s[0][0], s[0][1]), max_of(s[0][2], s[0][3])), max_of(max_of(s[1][0], s[1][1]), max_of(s[1][2], s[1][3])));
+      float top = max_of(max_of(s[0][0], s[0][1], s[0][2]), max_of(s[0][3], s[1][0], s[1][1]), max_of(s[1][2], s[1][3]));
       {
         float y = top;
         swap_lanes<16>(top, y);
@@ -362,10 +378,6 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], sl2, minus));
         l += p[i];
         if constexpr (kE4m3) p[i] *= power_of(v_exp[i / 4], i % 4);
-      }
-      if (kE4m3 && masked) {                      // no row, no exponent
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = 4 * g + i % 4 < now.rows[i / 4] ? p[i] : 0.f;
       }
       const u32x4 pw = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
       const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
@@ -571,10 +583,10 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const Pag
 constexpr int kCus = 256;
 static_assert(kCus * 2 <= kPagedMostWorkgroups, "room for the weights of pieces");
 // A workgroup of its own for every sequence and KV head: where no sequence can have more keys than this, by the width of the table; more
-// where there are so many that all CUs have one.  8 KV heads, d 128, e4m3, alone and in shares: one sequence of 512 keys 5.9 and 8.6 us, 768 7.4
-// and 8.6, 1024 8.9 and 8.7; 32 sequences of 512 7.2 and 12.2, of 1000 13.4 and 17.7, of 2500 27.4 and 32.3, of 44 to 2176 14.4 and 16.3; of 2500 once and
-// 300 else 15.4 and 11.8.
-constexpr long long kAloneKeys = 768, kAloneKeysOfMany = 2560;
+// where there are so many that all CUs have one.  8 KV heads, d 128, e4m3, alone and in shares: one sequence of 512 keys 5.7 and 8.5 us, 1024 7.5
+// and 8.7, 1280 8.7 and 8.8, 1536 9.7 and 8.9 (bf16 5.7 and 8.6, 7.7 and 8.8, 8.6 and 8.8, 9.5 and 8.8); 32 sequences of 512 7.1 and 12.2, of 1000 13.3 and
+// 17.9, of 2500 27.1 and 31.5, of 4000 43.4 and 46.9; of 2500 once and 300 else 13.6 and 11.8, of 4000 once 19.4 and 12.3.
+constexpr long long kAloneKeys = 1280, kAloneKeysOfMany = 2560;
 
 template <int D, bool kE4m3>
 hipError_t launch(const PagedDecodeArgs& a, hipStream_t s) {

@@ -260,6 +260,40 @@ def test_refusals():
 
 
 @gpu
+@pytest.mark.parametrize("e4m3,page", [(False, 16), (True, 256)])
+def test_pieces_of_many_tiles(e4m3, page):
+    """More than 32 tiles of 256 keys to a workgroup, behind a sequence of another length."""
+    gen = torch.Generator(device=DEV).manual_seed(page)
+    heads, d, lengths = 32, 128, [300, 135001 if e4m3 else 70001]
+    counts = [-(-n // page) for n in lengths]
+    pages = K.Pages.empty(sum(counts), heads, d, page, e4m3, DEV)
+    if e4m3:
+        for t, exp in ((pages.k, pages.k_exp), (pages.v, pages.v_exp)):
+            t.view(torch.uint8).random_(0, 0x7F, generator=gen)          # every number that is one, not negative
+            exp.random_(117, 121, generator=gen)
+    else:
+        pages.k.normal_(generator=gen), pages.v.normal_(generator=gen)
+    order = torch.randperm(sum(counts), generator=gen, device=DEV).int()
+    table = torch.full((2, counts[1]), -1, dtype=torch.int32, device=DEV)
+    table[0, :counts[0]], table[1] = order[:counts[0]], order[counts[0]:]
+    q = torch.randn(2, heads, d, generator=gen, device=DEV).to(torch.bfloat16)
+    out = pages.decode(q, table, int32(lengths))
+    torch.cuda.synchronize()
+    ref, size, most = torch.zeros(2, heads, d, dtype=torch.float64), torch.zeros(2, heads, d, dtype=torch.float64), 0.0
+    for s, n in enumerate(lengths):
+        mine = table[s, :counts[s]].long()
+        for h in range(heads):
+            k, v = (x[mine, h].double().view(-1, d)[:n] for x in (pages.k, pages.v))
+            if e4m3:
+                k, v = (x * torch.exp2(e[mine, h].double() - 127).view(-1, 1)[:n] for x, e in ((k, pages.k_exp), (v, pages.v_exp)))
+            one = q[s, h].double()
+            w = torch.softmax((k * one).sum(-1) * d ** -0.5, 0)[:, None]
+            ref[s, h], size[s, h] = (w * v).sum(0).cpu(), (w * v.abs()).sum(0).cpu()
+            most = max(most, float((k.abs() * one.abs()).sum(-1).max()) * d ** -0.5)
+    check(out, ref.numpy(), size.numpy(), most, d)
+
+
+@gpu
 def test_refusals_of_tensors():
     pages = K.Pages.empty(4, 2, 128, 64, False, DEV)
     row = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16, device=DEV)
