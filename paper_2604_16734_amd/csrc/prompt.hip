@@ -1,7 +1,7 @@
 // Causal attention inside each of many prompts that lie one behind the other (kvp_prompt_attention), for gfx950: bf16 MFMA 32x32x16, K
 // and V tiles through LDS.
 //
-// Bound by the matrix cores for long prompts: 4 d flops for each pair of a row and a key that it sees, against 2 d numbers of K and V that serve
+// Bound by the matrix cores for long prompts (16640 rows of 32/8 heads, d 128, 1873 us, 1210 TFLOP/s; a large library product here 1365): 4 d flops for each pair of a row and a key that it sees, against 2 d numbers of K and V that serve
 // the 128 rows of a workgroup and come out of the L2 cache of its die.
 //
 // Formulation.  A wave owns 32 query rows of one head and works on the transposed problem, S^T = K Q^T and O^T = V^T P^T: in the 32x32
@@ -9,8 +9,9 @@
 // accumulators are, register for register, the second operand of the second product.  Accumulator register r of lane (g = lane / 32) holds key
 // 8 (r / 4) + 4 g + r % 4 of its 32; V is read out of LDS, transposed, in that order of keys.
 //
-// A workgroup is four waves, 128 neighbouring rows of one head, and two of them share a CU: what one waits for the other fills.  Tiles of 64 keys come by
-// buffer_load ... lds into two K and two V buffers, 64 KiB, row by row with the 16-byte chunks of a row swizzled by its number, so that all
+// Many rows: a workgroup is four waves, 128 neighbouring rows of one head, and two of them share a CU (at d 64 three): what one waits for the other fills.
+// Or it is two groups of four waves for the same rows, which take the tiles in turns.  (Few rows, and short prompts: below.)  Tiles of 64 keys come by
+// buffer_load ... lds into two K and two V buffers of a group, row by row with the 16-byte chunks of a row swizzled by its number, so that all
 // reads are free of bank conflicts.  The descriptors end with the last row that a row of the workgroup sees: what lies behind it comes as zeros and costs
 // nothing.  Of tile t the wave takes the blocks of 32 keys X and Y; matrix and vector work overlap in program order:
 //   phase 1   MFMA: S_Y(t), O += P_Y(t-1) V     | vector: P_X(t) = exp(S_X(t) - m)
@@ -102,9 +103,10 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int rank, i
 struct Item {
   int rank, head;
 };
-__device__ __forceinline__ Item item_of(const PromptArgs& a) {
+// Item number `mine` of this workgroup's die.
+__device__ __forceinline__ Item item_of(const PromptArgs& a, unsigned mine) {
   const int xcd = blockIdx.x % kXcds, set = xcd / a.dies_per_set;
-  const unsigned item = blockIdx.x / kXcds * (unsigned)a.dies_per_set + (unsigned)(xcd - set * a.dies_per_set);
+  const unsigned item = mine * (unsigned)a.dies_per_set + (unsigned)(xcd - set * a.dies_per_set);
   const int rank = (int)quotient(item, a.by_set_heads);
   return Item{rank, set * a.set_heads + (int)item - rank * a.set_heads};
 }
@@ -174,6 +176,28 @@ __device__ __forceinline__ void rows_the_slow_way(const bf16x8 (&qf)[D / 16], co
   }
 }
 
+// rows of a wave to memory, through 32 of its rows of LDS so that the stores are whole rows
+template <int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float inv, u32x4* rows, u16* to, long long to_token, int n_rows, int lane) {
+  constexpr int kChunks = D / 8;
+  const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {        // fours j of a channel tile are its channels 8 j + 4 g .. + 3: the halves of the wave exchange one of two
+      const f32x16& x = o[dt];
+      const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j] * inv, x[4 * j + 1] * inv), pack_bf16(x[4 * j + 4] * inv, x[4 * j + 5] * inv), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j + 2] * inv, x[4 * j + 3] * inv), pack_bf16(x[4 * j + 6] * inv, x[4 * j + 7] * inv), false, false);
+      rows[l32 * kChunks + ((4 * dt + j + g) ^ k_swizzle<D>(l32))] = u32x4{lo[0], hi[0], lo[1], hi[1]};
+    }
+#pragma unroll
+  for (int it = 0; it < kChunks / 2; ++it) {
+    const int r = (64 * it + lane) / kChunks, ch = lane % kChunks;
+    const u32x4 val = rows[r * kChunks + (ch ^ k_swizzle<D>(r))];
+    if (r < n_rows) *reinterpret_cast<u32x4*>(to + (long long)r * to_token + 8 * ch) = val;
+  }
+}
+
 template <int D, int KS>
 __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerSimd)) prompt_kernel(const PromptArgs a) {
   using S = Shape<D, KS>;
@@ -184,7 +208,7 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
   u16* const lds_k = reinterpret_cast<u16*>(lds_raw + ks * S::kGroupLds);      // [2][kTile]
   u16* const lds_v = lds_k + 2 * S::kTile;                                     // [2][kTile]
 
-  const Item item = item_of(a);
+  const Item item = item_of(a, blockIdx.x / kXcds);
   const int rank = item.rank, h = item.head;
   const PromptTile pt = find_tile<kPromptRows>(a, rank, lane);
   const int n = pt.length, wg_row = pt.tile * kPromptRows;
@@ -524,50 +548,35 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
     rows_the_slow_way<D>(qf, k_rows, a.k_token, v_rows, a.v_token, q0, n, sl2, l32, g, o, l_row);
   }
 
-  // ---- rows to memory, through this wave's strip of LDS so that the stores are whole rows
-  const float inv = 1.f / l_row;
-  u32x4* const rows = reinterpret_cast<u32x4*>(lds_raw) + wave * 32 * S::kChunks;
-#pragma unroll
-  for (int dt = 0; dt < kND; ++dt)
-#pragma unroll
-    for (int j = 0; j < 4; j += 2) {        // fours j of a channel tile are its channels 8 j + 4 g .. + 3: the halves of the wave exchange one of two
-      const f32x16& x = o[dt];
-      const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j] * inv, x[4 * j + 1] * inv), pack_bf16(x[4 * j + 4] * inv, x[4 * j + 5] * inv), false, false);
-      const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * j + 2] * inv, x[4 * j + 3] * inv), pack_bf16(x[4 * j + 6] * inv, x[4 * j + 7] * inv), false, false);
-      rows[l32 * S::kChunks + ((4 * dt + j + g) ^ k_swizzle<D>(l32))] = u32x4{lo[0], hi[0], lo[1], hi[1]};
-    }
-#pragma unroll
-  for (int it = 0; it < S::kChunks / 2; ++it) {
-    const int r = (64 * it + lane) / S::kChunks, ch = lane % S::kChunks;
-    const u32x4 val = rows[r * S::kChunks + (ch ^ k_swizzle<D>(r))];
-    if (q0 + r < n) *reinterpret_cast<u32x4*>(out_rows + (long long)(q0 + r) * a.out_token + 8 * ch) = val;
-  }
+  store_rows<D>(o, 1.f / l_row, reinterpret_cast<u32x4*>(lds_raw) + wave * 32 * S::kChunks, out_rows + (long long)q0 * a.out_token, a.out_token, n - q0, lane);
 }
 
 // ---- Few rows: workgroups of 128 would leave most of the chip idle and each have a long way to go.  Here one has 32 rows of one head, and its eight waves
 // share the keys, every eighth block of 32 each, as they come through two strips of LDS of the wave's own: no barrier between the query rows and
 // the end, where the waves' results are added up.  Bound by latency: the loads, a block or a few, and the sum over the waves.
-template <int D>
+// Short prompts: the same with each of four waves at 32 rows of its own, for which it goes through all keys by itself.
+template <int D, bool kShared>
 struct FewShape {
-  static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32;
+  static constexpr int kWaves = kShared ? 8 : 4, kThreads = 64 * kWaves, kRows = 32;
+  static constexpr int kItems = kShared ? 1 : kWaves;          // tiles of a workgroup
   static constexpr int kChunks = D / 8, kRowsPerLoad = 64 / kChunks;
   static constexpr int kLoads = 16 / kRowsPerLoad;             // for 16 rows
   static constexpr int kStrip = 32 * D;                        // numbers: 32 keys
   static constexpr int kWaveBytes = 2 * kStrip * 2;            // K, V; then what the wave leaves of its rows, as it is in the accumulators
-  static constexpr int kQ = kWaves * kWaveBytes, kStat = kQ + kRows * D * 2;
-  static constexpr int kLds = kStat + kWaves * 2 * kRows * 4;
+  static constexpr int kQ = kWaves * kWaveBytes, kStat = kQ + kRows * D * 2;      // (shared)
+  static constexpr int kLds = kShared ? kStat + kWaves * 2 * kRows * 4 : kQ;
   static constexpr unsigned kPerCu = kLds > 80 * 1024 ? 1 : 2;
   static_assert(kRows * D * 4 <= kWaveBytes && kLds <= 160 * 1024, "LDS of a CU");
 };
 
-template <int D>
-__global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(const PromptArgs a) {
-  using S = FewShape<D>;
+template <int D, bool kShared>
+__global__ void __launch_bounds__((FewShape<D, kShared>::kThreads), 2) prompt_few_kernel(const PromptArgs a) {
+  using S = FewShape<D, kShared>;
   constexpr int kNK = D / 16, kNV = (D / 32) * 2, kND = D / 32;
   extern __shared__ __align__(16) unsigned char lds_raw[];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Item item = item_of(a);
+  const Item item = item_of(a, blockIdx.x / kXcds * S::kItems + (kShared ? 0 : wave));
   const PromptTile pt = find_tile<S::kRows>(a, item.rank, lane);
   const int n = pt.length, q0 = pt.tile * S::kRows, h = item.head;
   if (q0 >= n) return;
@@ -632,23 +641,6 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
   typedef std::integral_constant<int, 4 * S::kLoads> BothStrips;
   typedef std::integral_constant<int, 0> None;
 
-  // the query rows: a load of each wave (of the first four at d 64), for all; the wave's first block behind it
-  if (wave < 32 / S::kRowsPerLoad) {
-    const int row0 = S::kRowsPerLoad * wave, row = row0 + ld_sub;
-    const unsigned long long at = (unsigned long long)(q_rows + (long long)(q0 + row0) * a.q_token);
-    const u32x4 buffer = {(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xFFFFu,
-                          (unsigned)__builtin_amdgcn_readfirstlane((int)bytes_of_rows<D>(n - q0 - row0, S::kRowsPerLoad, a.q_bytes)), 0x00020000u};
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"((unsigned)ld_sub * a.q_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row))),
-                 "s"(buffer), "s"(lds_at + (unsigned)(S::kQ + 1024 * wave))
-                 : "m0", "memory");
-  }
-  if (wave < n_blocks) {
-    issue_k(wave);
-    issue_v(wave);
-    wait_all_but(BothStrips{});
-  } else {
-    wait_all_but(None{});
-  }
   int k_off[kNK], v_off[kND];
 #pragma unroll
   for (int st = 0; st < kNK; ++st) k_off[st] = l32 * D + 8 * ((2 * st) ^ (g ^ k_swizzle<D>(l32)));
@@ -657,18 +649,50 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
 #pragma unroll
     for (int dt = 0; dt < kND; ++dt) v_off[dt] = rsub * D + 8 * ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ z) + 4 * (lane & 1);
   }
-  __syncthreads();
   bf16x8 qf[kNK];
+  auto load_q = [&](int row0, unsigned to) __attribute__((always_inline)) {              // kRowsPerLoad rows
+    const int row = row0 + ld_sub;
+    const unsigned long long at = (unsigned long long)(q_rows + (long long)(q0 + row0) * a.q_token);
+    const u32x4 buffer = {(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xFFFFu,
+                          (unsigned)__builtin_amdgcn_readfirstlane((int)bytes_of_rows<D>(n - q0 - row0, S::kRowsPerLoad, a.q_bytes)), 0x00020000u};
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"((unsigned)ld_sub * a.q_bytes + 16u * (unsigned)(ld_pos ^ k_swizzle<D>(row))),
+                 "s"(buffer), "s"(to)
+                 : "m0", "memory");
+  };
+  if constexpr (kShared) {
+    // the query rows: a load of each wave (of the first four at d 64), for all; the wave's first block behind it
+    if (wave < 32 / S::kRowsPerLoad) load_q(S::kRowsPerLoad * wave, lds_at + (unsigned)(S::kQ + 1024 * wave));
+    if (wave < n_blocks) {
+      issue_k(wave);
+      issue_v(wave);
+      wait_all_but(BothStrips{});
+    } else {
+      wait_all_but(None{});
+    }
+    __syncthreads();
 #pragma unroll
-  for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(q_lds + k_off[st]);
+    for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(q_lds + k_off[st]);
+  } else {
+    // the query rows through the strip of V, beside the first keys
+#pragma unroll
+    for (int j = 0; j < 32 / S::kRowsPerLoad; ++j) load_q(S::kRowsPerLoad * j, my_lds + 2u * (unsigned)S::kStrip + 1024u * j);
+    issue_k(0);
+    wait_all_but(OneStrip{});
+#pragma unroll
+    for (int st = 0; st < kNK; ++st) qf[st] = lds_read_b128(v_strip + k_off[st]);
+#pragma unroll
+    for (int st = 0; st < kNK; ++st) asm volatile("" : "+v"(qf[st]));    // read, before the strip is filled
+    issue_v(0);
+  }
 
   f32x16 o[kND];
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int dt = 0; dt < kND; ++dt) o[dt] = zero;
   float m = -INFINITY, l = 0.f;
-  for (int b = wave; b < n_blocks; b += S::kWaves) {
-    const bool more = b + S::kWaves < n_blocks;
+  constexpr int kStep = kShared ? S::kWaves : 1;
+  for (int b = kShared ? wave : 0; b < n_blocks; b += kStep) {
+    const bool more = b + kStep < n_blocks;
     wait_all_but(OneStrip{});
     f32x16 s = zero;
 #pragma unroll
@@ -676,7 +700,7 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
     // K has been read; and a vector instruction may read a product 12 wait states after it, which the compiler does not see to in
     // another basic block
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_nop 7" : "+v"(s)::"memory");
-    if (more) issue_k(b + S::kWaves);
+    if (more) issue_k(b + kStep);
     if (b == n_blocks - 1) {                   // key 8 (r / 4) + 4 g + r % 4 of the block and row l32 of the tile
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) <= l32 - 4 * g ? s[r] : -INFINITY;
@@ -708,12 +732,23 @@ __global__ void __launch_bounds__((FewShape<D>::kThreads), 2) prompt_few_kernel(
       o[vi / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read_vt(v_strip + v_off[vi / 2] + 16 * (vi % 2) * D, 8 * D), __builtin_bit_cast(bf16x8, pw), o[vi / 2], 0, 0, 0);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) issue_v(b + S::kWaves);
+    if (more) issue_v(b + kStep);
   }
 
-  // ---- the waves' results, added up: a thread has eight channels of a row
   if constexpr (kND == 4) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]));
   else asm volatile("s_nop 7\n\ts_nop 7" : "+v"(o[0]), "+v"(o[1]));
+  if constexpr (!kShared) {
+    float l_row = sum_with_other_half(l), check = l_row * 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kND; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[dt][r], 0.f, check);
+    // what is not finite is not 0 when it is multiplied by 0: a value that the row does not see may be in it
+    if (__any(!(check == 0.f))) rows_the_slow_way<D>(qf, k_rows, a.k_token, v_rows, a.v_token, q0, n, sl2, l32, g, o, l_row);
+    store_rows<D>(o, 1.f / l_row, reinterpret_cast<u32x4*>(k_strip), out_rows + (long long)q0 * a.out_token, a.out_token, n - q0, lane);
+    return;
+  }
+  // ---- the waves' results, added up: a thread has eight channels of a row
   if (wave < n_blocks) {
     l = sum_with_other_half(l);
     if (g == 0) {
@@ -761,37 +796,50 @@ template <int D, int KS>
 hipError_t prepare() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_kernel<D, KS>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape<D, KS>::kLds);
 }
-template <int D>
+template <int D, bool kShared>
 hipError_t prepare_few() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_few_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kLds);
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_few_kernel<D, kShared>), hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D, kShared>::kLds);
 }
 
-// The grid for tiles of so many rows: every prompt may have one that is not full.
-unsigned deal_out(PromptArgs& a, int rows) {
+// The grid for tiles of so many rows, `each` of them to a workgroup: every prompt may have one that is not full.
+unsigned deal_out(PromptArgs& a, int rows, int each) {
   const long long tiles = ((long long)a.n_tokens + (long long)(rows - 1) * a.n_seqs) / rows;
   const unsigned items = (unsigned)(tiles * a.set_heads), per_die = (items + a.dies_per_set - 1) / a.dies_per_set;
-  a.by_set_heads = divisor_of((unsigned)a.set_heads, items + kXcds);
-  return kXcds * per_die;
+  a.by_set_heads = divisor_of((unsigned)a.set_heads, items + (unsigned)(each * kXcds));
+  return kXcds * ((per_die + each - 1) / each);
 }
 
-// Three ways, by the workgroups that there would be and the mean length of the prompts.
-// 32 rows: while the chip holds all of these workgroups at once, one per CU at d 128 and two at 64, or twice as many of long prompts.  Against 128 rows,
-// d 128: 4 heads of 608 rows (76 workgroups) 8.3 and 11.6 us, 32 of 256 (256) 6.8 and 8.5, 32 of 384 (384) 10.7 and 10.4, 16 of 1024 (512) 15.9 and 16.1, 8 of
-// 2000 (504) 21.3 and 24.2, 8 of eight prompts of 200 (448) 10.6 and 8.3; d 64: 32 of 512 (512) 7.5 and 8.2, 32 of 640 (640) 10.5 and 9.3.
+template <int D, bool kShared>
+hipError_t launch_few(const PromptArgs& a, unsigned grid, hipStream_t s) {
+  using S = FewShape<D, kShared>;
+  hipLaunchKernelGGL((prompt_few_kernel<D, kShared>), dim3(grid), dim3(S::kThreads), S::kLds, s, a);
+  return hipGetLastError();
+}
+
+// Four ways, by the workgroups that there would be and the mean length of the prompts; the host knows no other.
+// 32 rows by eight waves: while the chip holds all of these workgroups at once, one per CU at d 128 and two at 64, or a quarter more, or 512 of long
+// prompts.  Against 128 rows, d 128: 4 heads of 608 rows (76 workgroups) 8.3 and 11.6 us, 32 of 256 (256) 6.8 and 8.5, 4 of eight prompts of 295 (324) 9.6 and
+// 9.1, of one of 1562 and seven of 100 (312) 14.6 and 20.0, 16 of 1024 (512) 15.9 and 16.1, 8 of 2000 (504) 21.3 and 24.2, 8 of eight prompts of 200 (448)
+// 10.6 and 8.3; d 64: 32 of 512 (512) 7.5 and 8.2, 8 of one of 1562 and seven of 100 (624) 12.4 and 15.5, 4 of 32 prompts of 128 (636) 6.5 and 5.9.
+// 32 rows by one wave: short prompts, where 128 rows would be more workgroups than the chip holds, most of each idle.  32/8 heads, d 128, 128 rows and 32: 56
+// prompts of one row 19.7 and 6.7 us, 28 of 26 12.0 and 6.2, 64 of 64 28.7 and 22.2, 26 of 100 19.2 and 17.3; 60 of 30 and one of 1000 36.1 and 36.4, of
+// 2000 57.5 and 66.7; d 64 64 of 64 17.1 and 10.7, 60 of 30 and one of 2000 34.4 and 51.4.
 // 128 rows and two groups of waves that share the keys: where every workgroup has a CU to itself (a wave alone on a SIMD has the pipe wait for it half of
 // the time), or nearly so and the longest of them decides, and the prompts are not too short for it.  One group and two, d 128: 32 heads of 512 rows
-// 12.3 and 11.9 us, 1536 30.3 and 27.4, 4096 132 and 136, 8 of 8000 (504 workgroups) 138 and 122, 4 of 16000 (500) 270 and 233, 16 of eight prompts of 500
-// (512) 18.0 and 23.7; d 64, 4 of 16000 170 and 150.
+// 12.3 and 11.9 us, 1536 30.3 and 27.4, 4096 132 and 136, 8 of 8000 (504 workgroups) 138 and 122, 4 of 16000 (500) 270 and 233, 8 of one prompt of 1562 and
+// seven of 100 (200) 23.9 and 20.5, of eight of 295 (208) 9.4 and 10.2, 16 of eight of 500 (512) 18.0 and 23.7; d 64, 4 of 16000 170 and 150.
 template <int D>
 hipError_t launch(PromptArgs a, hipStream_t s) {
   const long long mean = a.n_tokens / a.n_seqs;
-  unsigned grid = deal_out(a, FewShape<D>::kRows);
-  if (grid <= 256 * FewShape<D>::kPerCu || (grid <= 512 && mean >= 1024)) {
-    hipLaunchKernelGGL(prompt_few_kernel<D>, dim3(grid), dim3(FewShape<D>::kThreads), FewShape<D>::kLds, s, a);
-    return hipGetLastError();
+  constexpr unsigned kFew = 256 * FewShape<D, true>::kPerCu;
+  unsigned grid = deal_out(a, 32, 1);
+  if (grid <= kFew + kFew / 4 || (grid <= 512 && mean >= 1024)) return launch_few<D, true>(a, grid, s);
+  grid = deal_out(a, kPromptRows, 1);
+  if (grid > 512 && mean <= 64) {
+    grid = deal_out(a, 32, FewShape<D, false>::kItems);
+    return launch_few<D, false>(a, grid, s);
   }
-  grid = deal_out(a, kPromptRows);
-  if ((grid <= 256 && mean >= 384) || (grid <= 512 && mean >= 1024))
+  if ((grid <= 256 && mean >= 192) || (grid <= 512 && mean >= 1024))
     hipLaunchKernelGGL((prompt_kernel<D, 2>), dim3(grid), dim3(Shape<D, 2>::kThreads), (Shape<D, 2>::kLds), s, a);
   else
     hipLaunchKernelGGL((prompt_kernel<D, 1>), dim3(grid), dim3(Shape<D, 1>::kThreads), (Shape<D, 1>::kLds), s, a);
@@ -803,8 +851,9 @@ hipError_t launch(PromptArgs a, hipStream_t s) {
 hipError_t prepare_prompt() {
   hipError_t e;
   if ((e = prepare<128, 1>()) != hipSuccess || (e = prepare<128, 2>()) != hipSuccess || (e = prepare<64, 1>()) != hipSuccess) return e;
-  if ((e = prepare<64, 2>()) != hipSuccess || (e = prepare_few<64>()) != hipSuccess) return e;
-  return prepare_few<128>();
+  if ((e = prepare<64, 2>()) != hipSuccess || (e = prepare_few<64, true>()) != hipSuccess || (e = prepare_few<64, false>()) != hipSuccess) return e;
+  if ((e = prepare_few<128, true>()) != hipSuccess) return e;
+  return prepare_few<128, false>();
 }
 
 hipError_t launch_prompt(const PromptArgs& a, int head_dim, hipStream_t s) { return head_dim == 128 ? launch<128>(a, s) : launch<64>(a, s); }

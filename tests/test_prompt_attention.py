@@ -113,6 +113,39 @@ def test_many_prompts():
     same(out, ref, size, most, 64)
 
 
+@gpu
+@pytest.mark.parametrize("how", ["rows", "projection"])
+@pytest.mark.parametrize("hq,hkv,d", [(16, 4, 128), (28, 4, 64), (32, 32, 128), (20, 20, 64)])
+def test_short_prompts(hq, hkv, d, how):
+    """Many of a few rows and one longer one; rows around them with NaNs, large logits, first keys that weigh nothing, and values that only the last
+    row of a prompt sees."""
+    gen = torch.Generator().manual_seed(hq + d)
+    lengths = [0, 1, 2, 31, 32, 33, 63, 64, 65, 300, 0] + [int(x) for x in torch.randint(1, 60, (40,), generator=gen)] + [17]
+    begin = (np.concatenate([[0], np.cumsum(lengths)]) + 2).tolist()
+    n = begin[-1] + 3
+    q, k, v = randn(gen, n, hq, d, scale=1.5), randn(gen, n, hkv, d), randn(gen, n, hkv, d)
+    q[begin[20]:begin[24]] *= 32
+    k[begin[9]:begin[9] + 40] = -math.inf
+    q[begin[9]:begin[10]] = q[begin[9]:begin[10]].abs() + 0.125
+    k[begin[9] + 40:begin[10]] = -k[begin[9] + 40:begin[10]].abs() - 0.5
+    last = [begin[i + 1] - 1 for i in range(12, len(lengths))]
+    v[last] = math.inf
+    k[:2], v[:2], k[begin[-1]:], v[begin[-1]:] = (float("nan"),) * 4
+    (qd, _), (kd, _), (vd, _) = (laid_out(x, how) for x in (q, k, v))
+    out, room = laid_out(torch.full_like(q, 7.0), how)
+    print("short prompts", hq, hkv, d, how, flush=True)
+    K.prompt_attention(qd, kd, vd, int32(begin), out=out)
+    torch.cuda.synchronize()
+    clean = v.clone()
+    clean[last] = 0.0
+    ref, size, most = causal(q, k, clean, begin, d ** -0.5)
+    ref[last], ref[begin[9]:begin[9] + 40] = math.nan, math.nan
+    assert np.isfinite(ref).all(axis=(1, 2)).sum() == sum(lengths) - len(last) - 40
+    same(out, ref, size, most, d)
+    assert not torch.isfinite(out[last]).any()
+    assert (out[:2] == 7).all() and (out[begin[-1]:] == 7).all()
+
+
 # few rows for the chip, many, and many of few heads
 @gpu
 @pytest.mark.parametrize("n,hq,hkv", [(450, 4, 2), (450, 96, 48), (900, 24, 12)])
@@ -190,11 +223,12 @@ def test_bounds_out_of_range():
 
 @gpu
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (96, 24, 64), (96, 8, 128)])
-def test_prompts_on_another_stream_and_in_a_graph(hq, hkv, d):
+@pytest.mark.parametrize("empty", [0, 30])
+def test_prompts_on_another_stream_and_in_a_graph(hq, hkv, d, empty):
     gen = torch.Generator().manual_seed(6)
     n = 500
     q, k, v = (x.to(DEV) for x in (randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)))
-    begin, out = int32([0, 100, 500]), torch.zeros_like(q)
+    begin, out = int32([0] * empty + [0, 100, 500]), torch.zeros_like(q)
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
     other = K.prompt_attention(q, k, v, begin, stream=side)
@@ -203,7 +237,7 @@ def test_prompts_on_another_stream_and_in_a_graph(hq, hkv, d):
     with torch.cuda.graph(graph):
         K.prompt_attention(q, k, v, begin, out=out)
     for bounds in ([0, 100, 500], [0, 400, 500], [0, 0, 490], [0, 250, 250]):
-        begin.copy_(int32(bounds))
+        begin.copy_(int32([bounds[0]] * empty + bounds))
         out.fill_(7.0)
         graph.replay()
         eager = K.prompt_attention(q, k, v, begin, out=torch.full_like(q, 7.0))
