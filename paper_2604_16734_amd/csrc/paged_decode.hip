@@ -476,7 +476,7 @@ __device__ __forceinline__ Pieces pieces_of(const PagedDecodeArgs& a, int seq, i
   return p;
 }
 
-// Many sequences: a wave for each query head of one.  (96 sequences, 32/8 heads, d 128: 15.8 us with the kernel below, 5.0 this way.)
+// Many sequences: a wave for each query head of one.  (96 sequences, 32/8 heads, d 128: 15.8 us with the kernel below, 4.9 this way.)
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDecodeArgs a) {
   constexpr int kLanes = D / 4, kSlots = 64 / kLanes;
@@ -490,6 +490,10 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDec
   const float* const stats = a.partial + (size_t)2 * a.workgroups * a.group * D;
   auto slot_of = [&](unsigned i) __attribute__((always_inline)) { return (size_t)piece_slot(p.first, p.w0 + i, p.share) * a.group + column; };
   const int sub = lane / kLanes, piece = lane % kLanes;
+  constexpr int kFirst = 4;
+  f32x4 first[kFirst];                         // beside the maxima and sums, not after them
+#pragma unroll
+  for (int j = 0; j < kFirst; ++j) first[j] = *reinterpret_cast<const f32x4*>(a.partial + slot_of(min((unsigned)(sub + kSlots * j), p.n - 1)) * D + 4 * piece);
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (unsigned base = 0; base < p.n; base += 64) {
@@ -502,11 +506,18 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDec
     m = most;
     l = l * by + over_wave(f * sum, FloatSum{});
     o *= by;
-#pragma unroll 4
-    for (unsigned i = sub; i < (here + kSlots - 1) / kSlots * kSlots; i += kSlots) {      // (all lanes: the last ones again, with weight 0)
+    auto add = [&](unsigned i, const f32x4& row) __attribute__((always_inline)) {      // (all lanes)
       const float w = __shfl(f, (int)i);
-      o += w * *reinterpret_cast<const f32x4*>(a.partial + slot_of(base + min(i, here - 1)) * D + 4 * piece);
+      if (i < here) o += w * row;
+    };
+    unsigned i = sub;
+    if (base == 0) {
+#pragma unroll
+      for (int j = 0; j < kFirst; ++j) add(sub + kSlots * j, first[j]);
+      i += kSlots * kFirst;
     }
+#pragma unroll 4
+    for (; i < (here + kSlots - 1) / kSlots * kSlots; i += kSlots) add(i, *reinterpret_cast<const f32x4*>(a.partial + slot_of(base + min(i, here - 1)) * D + 4 * piece));
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -524,7 +535,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDec
 }
 
 // Few sequences, each in many pieces: four waves share the pieces of one query head, and a workgroup takes kJoinChannels of its channels.
-// (131071 keys of 28/4 heads: 14.8 us with all channels to a workgroup and one loop of dependent loads, 4.9 this way.)
+// (131071 keys of 28/4 heads: 14.8 us with all channels to a workgroup and one loop of dependent loads, 4.9 with weights first, 3.9 this way.)
 constexpr int kJoinChannels = 32;
 
 template <int D>
@@ -541,11 +552,22 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const Pag
   const unsigned n = p.n;
   const float* const stats = a.partial + (size_t)2 * a.workgroups * a.group * D;
   auto slot_of = [&](unsigned i) __attribute__((always_inline)) { return (size_t)piece_slot(p.first, p.w0 + i, p.share) * a.group + column; };
-  float top = -INFINITY;
-  for (unsigned i = tid; i < n; i += kJoinThreads) {
-    weights[i] = stats[2 * slot_of(i)];
-    top = fmaxf(top, weights[i]);
+  // maxima, sums and the first rows in one trip to memory
+  constexpr int kMine = kPagedMostWorkgroups / kJoinThreads, kRows = 8;
+  f32x2 stat[kMine];
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const unsigned i = tid + kJoinThreads * j;
+    stat[j] = i < n ? *reinterpret_cast<const f32x2*>(stats + 2 * slot_of(i)) : f32x2{-INFINITY, 0.f};
   }
+  const int sub = tid / kLanes, piece = tid % kLanes;
+  const float* const at = a.partial + kJoinChannels * blockIdx.z + 4 * piece;
+  f32x4 first[kRows];
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) first[j] = *reinterpret_cast<const f32x4*>(at + slot_of(min(sub + kSlots * j, (int)n - 1)) * D);
+  float top = stat[0][0];
+#pragma unroll
+  for (int j = 1; j < kMine; ++j) top = fmaxf(top, stat[j][0]);
   top = over_wave(top, FloatMax{});
   if (lane == 0) tops[wave] = top;
   __syncthreads();
@@ -554,19 +576,21 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const Pag
   for (int w = 1; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
   const float use = top == -INFINITY ? 0.f : top;
   float total = 0.f;
-  for (unsigned i = tid; i < n; i += kJoinThreads) {
-    const float f = __builtin_amdgcn_exp2f(weights[i] - use);
-    total += f * stats[2 * slot_of(i) + 1];
-    weights[i] = f;
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const float f = __builtin_amdgcn_exp2f(stat[j][0] - use);
+    total += f * stat[j][1];
+    weights[tid + kJoinThreads * j] = f;                 // 0 where there is no piece
   }
   total = over_wave(total, FloatSum{});
   if (lane == 0) sums[wave] = total;
   __syncthreads();
-  const int sub = tid / kLanes, piece = tid % kLanes;
-  const float* const at = a.partial + kJoinChannels * blockIdx.z + 4 * piece;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kRows; ++j)
+    if (sub + kSlots * j < (int)n) o += weights[sub + kSlots * j] * first[j];
 #pragma unroll 8
-  for (unsigned i = sub; i < n; i += kSlots) o += weights[i] * *reinterpret_cast<const f32x4*>(at + slot_of(i) * D);
+  for (unsigned i = sub + kSlots * kRows; i < n; i += kSlots) o += weights[i] * *reinterpret_cast<const f32x4*>(at + slot_of(i) * D);
   rows[sub][piece] = o;
   __syncthreads();
   if (tid >= kLanes) return;
