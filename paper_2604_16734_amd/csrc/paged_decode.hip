@@ -1,7 +1,8 @@
 // One decode step of many sequences, each over its own pages (kvp_paged_decode): out = softmax(scale q K^T) V with one query row per
 // query head.
 //
-// Bound by HBM: every key and value is read once and meets the G query heads of its KV head, 4 G flops for two numbers.  So what counts is
+// Bound by HBM (96 sequences of up to 16640 keys, 32/8 heads, d 128, bf16: 313 us, 5.75 TB/s, what a copy reaches): every key and value is read once
+// and meets the G query heads of its KV head, 4 G flops for two numbers.  So what counts is
 // that every CU has loads on their way all the time, and that none of them has more to do than the others.
 //
 // Who does what.  The lengths are on the device, and the host plans nothing: pages.h deals the units of all sequences, tiles of 256 keys of
@@ -535,7 +536,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDec
 }
 
 // Few sequences, each in many pieces: four waves share the pieces of one query head, and a workgroup takes kJoinChannels of its channels.
-// (131071 keys of 28/4 heads: 14.8 us with all channels to a workgroup and one loop of dependent loads, 4.9 with weights first, 3.9 this way.)
+// (131071 keys of 28/4 heads: 14.8 us with all channels to a workgroup and one loop of dependent loads, 4.8 with weights first, 4.0 this way.)
 constexpr int kJoinChannels = 32;
 
 template <int D>
