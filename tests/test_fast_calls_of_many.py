@@ -1,0 +1,118 @@
+"""The native way of the calls of many sequences: what it hands on, and what it leaves to Python, for tensors on the CPU and an entry point that
+only looks at its arguments."""
+import ctypes
+import importlib.util
+import os
+
+import pytest
+import torch
+
+import paper_2604_16734_amd as K
+from paper_2604_16734_amd import build as build_module
+
+BF16 = torch.bfloat16
+P, I, L, F, Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+ROWS = ctypes.CFUNCTYPE(ctypes.c_int, P, ctypes.POINTER(K.KvpRows), P, P, I, P, I, P)
+DECODE = ctypes.CFUNCTYPE(ctypes.c_int, P, P, L, L, I, P, I, P, I, F, P, P, Z, P)
+PROMPT = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.POINTER(K.KvpPrompts), P)
+
+
+@pytest.fixture(scope="module")
+def module(tmp_path_factory):
+    path = build_module.build_fast_calls(os.path.join(str(tmp_path_factory.mktemp("fast_calls")), "_fast_calls.so"),
+                                         ["KVP_TENSOR_DEVICE=c10::DeviceType::CPU"])
+    spec = importlib.util.spec_from_file_location("_fast_calls", path)
+    found = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(found)
+    return found
+
+
+def address(entry):
+    return ctypes.cast(entry, P).value
+
+
+def fields(struct):
+    return {name: getattr(struct, name) for name, _ in struct._fields_}
+
+
+def int32(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def left(call, good, others, taken):
+    """One argument at a time of a call that is taken."""
+    n = len(taken)
+    for at, values in others:
+        for other in values:
+            assert call(*(good[:at] + [other] + good[at + 1:])) is None, (at, other)
+    assert len(taken) == n
+    for wrong in (good[:-1], good + [None]):
+        with pytest.raises(TypeError):
+            call(*wrong)
+
+
+INTS = [None, 1.0, "1", 1 << 40]
+ADDRESSES = [None, "1", -1, 1 << 64]
+
+
+def rows_of(*shape):
+    return torch.zeros(*shape, dtype=BF16)
+
+
+def odd(x):
+    """Tensors unlike x [tokens, heads, d] in one respect."""
+    wide = torch.zeros(*x.shape[:2], 2 * x.shape[2], dtype=x.dtype)
+    return [None, x.float(), x[1:], x[:, 1:], x[..., :-64], x[None], x[0], wide[..., ::2], x.transpose(1, 2), x.to_sparse(), x.to("meta"), x.numpy]
+
+
+def test_rows(module):
+    taken = []
+    entry = ROWS(lambda pages, rows, begin, table, width, first, n_seqs, stream: taken.append((pages, fields(rows[0]), begin, table, width, first, n_seqs, stream)) or 7)
+    k, v = rows_of(3, 5, 128)[:, 1:3], rows_of(2, 9, 128)[:, :3].transpose(0, 1)
+    begin, table, first = int32(0, 1, 3), torch.zeros(2, 6, dtype=torch.int32), int32(4, 5)
+    good = [address(entry), 11, 2, 128, -1, 13, k, v, begin, table, first]
+    assert module.page_rows(*good) == 7
+    assert taken == [(11, dict(k=k.data_ptr(), v=v.data_ptr(), k_token=640, k_head=128, v_token=128, v_head=1152, n_tokens=3), begin.data_ptr(), table.data_ptr(), 6,
+                      first.data_ptr(), 2, 13)]
+    assert module.page_rows(*good[:-1], None) == 7 and taken[-1][5] is None
+    # distances of one token or head mean nothing; no tokens, no address
+    one = rows_of(1, 2, 128).as_strided((1, 2, 128), (3, 128, 1))
+    assert module.page_rows(*good[:6], one, one, begin, table, None) == 7 and taken[-1][1]["k_token"] == 0
+    none = rows_of(0, 2, 128)
+    assert module.page_rows(*good[:6], none, none, begin, table, None) == 7 and taken[-1][1]["n_tokens"] == 0 and taken[-1][1]["k"] is None
+    left(module.page_rows, good, [(0, ADDRESSES + [0]), (1, ADDRESSES + [0]), (2, INTS + [3]), (3, INTS + [64]), (4, INTS + [0]), (5, ADDRESSES), (6, odd(k)), (7, odd(v)),
+                                  (8, [None, begin[1:], begin.long(), int32(0, 0, 1, 1, 3, 3)[::2], begin[None]]),
+                                  (9, [None, table[1:], table[0], table.long(), torch.zeros(2, 7, dtype=torch.int32)[:, :6]]),
+                                  (10, [0, first[1:], first.long(), first[None], int32(1, 2, 3, 4)[::2]])], taken)
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_decode(module, own):
+    taken = []
+    entry = DECODE(lambda *args: taken.append(args) or 7)
+    q, out, table, lengths = rows_of(2, 9, 128)[:, :8:2], rows_of(2, 4, 128), torch.zeros(2, 6, dtype=torch.int32), int32(1, 2)
+    room = 4096 if own else torch.zeros(4096, dtype=torch.uint8)
+    good = [address(entry), 11, 4, 128, -1, 13, q, table, lengths, out, room, 0.25]
+    assert module.paged_decode(*good) == 7
+    assert taken[0][:11] == (11, q.data_ptr(), 1152, 256, 4, table.data_ptr(), 6, lengths.data_ptr(), 2, 0.25, out.data_ptr())
+    assert taken[0][12:] == (4096, 13) and (taken[0][11] == room.data_ptr() if not own else taken[0][11] % 16 == 0)
+    left(module.paged_decode, good, [(0, ADDRESSES + [0]), (1, ADDRESSES + [0]), (2, INTS + [3]), (3, INTS + [64]), (4, INTS + [0]), (5, ADDRESSES), (6, odd(q)),
+                                     (7, [None, table[1:], table[0], table.long(), torch.zeros(2, 7, dtype=torch.int32)[:, :6]]),
+                                     (8, [None, lengths[1:], lengths.long(), lengths[None], int32(1, 2, 3, 4)[::2]]), (9, odd(out) + [rows_of(4, 2, 128).transpose(0, 1)]),
+                                     (10, [None, 1.0, torch.zeros(64), torch.zeros(64, dtype=torch.uint8)[::2]]), (11, [None, 1, "1"])], taken)
+
+
+def test_prompt(module):
+    taken = []
+    entry = PROMPT(lambda prompts, stream: taken.append((fields(prompts[0]), stream)) or 7)
+    q, k, v, out = rows_of(3, 9, 64)[:, :8:2], rows_of(3, 2, 64), rows_of(2, 7, 64)[:, 2:5].transpose(0, 1), rows_of(4, 5, 64)[:, 1:4].transpose(0, 1)
+    begin = int32(0, 1, 3)
+    good = [address(entry), -1, 13, q, k, v, begin, out, 0.5]
+    assert module.prompt(*good) == 7
+    assert taken == [(dict(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), out=out.data_ptr(), seq_begin=begin.data_ptr(), q_token=576, q_head=128, k_token=128, k_head=64,
+                           v_token=64, v_head=448, out_token=64, out_head=320, n_tokens=3, n_seqs=2, n_q_heads=4, n_kv_heads=2, head_dim=64, softmax_scale=0.5), 13)]
+    wide = [rows_of(3, 4, 128), rows_of(3, 2, 128)]
+    left(module.prompt, good, [(0, ADDRESSES + [0]), (1, INTS + [0]), (2, ADDRESSES), (3, [q[1:], q[0], q.float(), wide[0], q.transpose(1, 2), None]),
+                               (4, [k[1:], k[0], k.float(), wide[1], rows_of(3, 4, 64), None]), (5, [v[1:], v[:, 1:], v.float(), wide[1], None]),
+                               (6, [None, begin.long(), begin[None], begin[:0], int32(0, 0, 1, 1, 3, 3)[::2]]),
+                               (7, [out[1:], out[:, 1:], out.float(), wide[0], None]), (8, [None, 1, "1"])], taken)
