@@ -23,27 +23,27 @@ constexpr int kThreads = 256;
 // A wave has kUnits times the rows that its lanes hold at once, for the price of one search for their places: 4, or 1 where all waves
 // run at once anyway.  (20 K tokens of 8 heads, d 128, to e4m3 25.4 us with 1 and a search for every row, 20.4 with 4; 48 tokens 3.4 and 4.2 us.)
 
-// The sequence of a token: the number of sequences that begin no later, less one.  One load and a vote per token for every 64 sequences;
-// lane i gets that of token from + i.  -1 or n_seqs: none.
-__device__ __forceinline__ int sequence_of(const int32_t* seq_begin, int n_seqs, int from, int to, int lane) {
-  int count = 0;
-  for (int base = 0; base <= n_seqs; base += 64) {
-    const bool any = base + lane <= n_seqs;
-    const int begin = any ? seq_begin[base + lane] : 0;
+// Where the first head's row of a token is in the pages: lane i's of token from + i.  The token's sequence is the number of those that begin no
+// later, less one; -1 or n_seqs: none.  One load and a vote per token for every 64 sequences.  What is needed of the sequence itself, where it begins and
+// its first place, comes out of the same load if there is only one (16640 rows of 8 heads into e4m3 pages 19.1 us with loads of their own behind it, 18.0
+// so; 48 rows 2.76 and 2.73), else out of loads behind it (300 sequences 3.3 us, 3.5 with what is needed passed on from group to group).
+constexpr long long kNoPlace = -1, kNoSequence = -2;
+__device__ __forceinline__ long long place_of_token(const PageRowsArgs& a, int from, int to, int lane) {
+  int count = 0, begin = 0, first = 0;
+  if (a.n_seqs < 64 && a.first != nullptr && lane < a.n_seqs) first = a.first[lane];
+  for (int base = 0; base <= a.n_seqs; base += 64) {
+    const bool any = base + lane <= a.n_seqs;
+    begin = any ? a.seq_begin[base + lane] : 0;
     for (int t = from; t <= to; ++t) {
       const int n = __popcll(__ballot(any && begin <= t));
       count += t == from + lane ? n : 0;
     }
   }
-  return count - 1;
-}
-
-// Where the first head's row of a token is in the pages: lane i's of token from + i.
-constexpr long long kNoPlace = -1, kNoSequence = -2;
-__device__ __forceinline__ long long place_of_token(const PageRowsArgs& a, int from, int to, int lane) {
-  const int seq = sequence_of(a.seq_begin, a.n_seqs, from, to, lane), token = from + lane;
+  const int seq = count - 1, token = from + lane;
+  if (a.n_seqs < 64) begin = __shfl(begin, max(seq, 0)), first = __shfl(first, max(seq, 0));
   if (token > to || seq < 0 || seq >= a.n_seqs) return kNoSequence;
-  const long long position = (long long)token - a.seq_begin[seq] + (a.first != nullptr ? a.first[seq] : 0);
+  if (a.n_seqs >= 64) begin = a.seq_begin[seq], first = a.first != nullptr ? a.first[seq] : 0;
+  const long long position = (long long)token - begin + first;
   if (!in_table(position, a.width, a.pool.shift)) return kNoPlace;
   const PagePlace at = place_of((int)position, a.pool.shift);
   const int page = a.table[(size_t)seq * a.width + at.column];
