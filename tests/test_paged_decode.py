@@ -260,6 +260,27 @@ def test_refusals():
 
 
 @gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("width", [4, 40])
+def test_pages_beyond_32_bits(e4m3, width):
+    """The last pages of a pool of more than 4 GiB give what the first ones of a small pool give, alone and in shares."""
+    gen = torch.Generator().manual_seed(width)
+    page, heads, d, n = 256, 8, 128, 900
+    many = (1 << 32) // (page * heads * d * (1 if e4m3 else 2)) + 5
+    k, v = (torch.randn(n, heads, d, generator=gen).to(torch.bfloat16).to(DEV) for _ in range(2))
+    q = torch.randn(1, 4 * heads, d, generator=gen).to(torch.bfloat16).to(DEV)
+    outs = []
+    for n_pages in (4, many):
+        pages = K.Pages.empty(n_pages, heads, d, page, e4m3, DEV)
+        table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+        table[0, :4] = torch.arange(n_pages - 1, n_pages - 5, -1)
+        pages.write(k, v, int32([0, n]), table)
+        outs.append(pages.decode(q, table, int32([n])))
+    torch.cuda.synchronize()
+    assert torch.equal(*outs) and outs[0].any()
+
+
+@gpu
 @pytest.mark.parametrize("e4m3,page", [(False, 16), (True, 256)])
 def test_pieces_of_many_tiles(e4m3, page):
     """More than 32 tiles of 256 keys to a workgroup, behind a sequence of another length."""

@@ -100,6 +100,28 @@ def test_strides(hq, hkv, d, how, other):
 
 
 @gpu
+@pytest.mark.parametrize("hq,lengths", [(4, [640, 60]), (48, [700]), (96, [640, 60]), (28, [16] * 43 + [12])])
+def test_rows_beyond_32_bits(hq, lengths):
+    """Rows 8 MiB apart: in every tensor the last ones lie 5.7 GB behind the first."""
+    gen = torch.Generator().manual_seed(hq)
+    n, hkv, d, far = sum(lengths), 2, 128, 1 << 22
+    begin = int32(np.concatenate([[0], np.cumsum(lengths)]).tolist())
+    q, k, v = (x.to(DEV) for x in (randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)))
+    plain = K.prompt_attention(q, k, v, begin)
+    room = torch.empty(n * far, dtype=torch.bfloat16, device=DEV)
+    at = 0
+    views = []
+    for x in (q, k, v, plain):
+        views.append(room.as_strided(x.shape, (far, d, 1), at))
+        at += x.shape[1] * d
+    for view, x in zip(views, (q, k, v)):
+        view.copy_(x)
+    K.prompt_attention(*views[:3], begin, out=views[3])
+    torch.cuda.synchronize()
+    assert torch.equal(views[3], plain)
+
+
+@gpu
 def test_many_prompts():
     gen = torch.Generator().manual_seed(2)
     lengths = [0] * 70 + [int(x) for x in torch.randint(0, 300, (90,), generator=gen)] + [0] * 40
