@@ -19,7 +19,7 @@
 //   phase 2   MFMA: S_X(t+1), O += P_X(t) V     | vector: P_Y(t) = exp(S_Y(t) - m), the loads of K(t+2) and V(t+1)
 //
 // Softmax reference.  exp(S - m) is exact for any m as long as nothing overflows: a row takes the maximum of the first 32 keys that it
-// sees and O is never rescaled.  A row sum beyond 2^64 says that this did not do, and minus infinity is no reference; a result that is not finite may also
+// sees (two groups: each its own, and so is its sum) and O is never rescaled.  A row sum beyond 2^64 says that this did not do, and minus infinity is no reference; a result that is not finite may also
 // come from a value that the row does not see, because 0 times infinity is no 0.  In these cases the wave takes its rows again the slow way, with a
 // running maximum and values only where they are seen.
 #include <type_traits>
@@ -525,9 +525,11 @@ __global__ void __launch_bounds__((Shape<D, KS>::kThreads), (Shape<D, KS>::kPerS
     }
     __syncthreads();
     if (ks == 1) return;
-    const float m_other = stat[l32], top = fmaxf(m_ref, m_other), use = top == -INFINITY ? 0.f : top;
+    const float m_other = stat[l32], l_other = stat[32 + l32], top = fmaxf(m_ref, m_other), use = top == -INFINITY ? 0.f : top;
     const float f0 = __builtin_amdgcn_exp2f((m_ref - use) * sl2), f1 = __builtin_amdgcn_exp2f((m_other - use) * sl2);
-    l_row = l_row * f0 + stat[32 + l32] * f1;
+    // (each sum by itself: the factor of a reference far below the other one is 0, which leaves out 2^64 2^-126 at most, not what is above)
+    const bool of_use = l_row <= 0x1p64f && l_other <= 0x1p64f;
+    l_row = of_use ? l_row * f0 + l_other * f1 : NAN;
 #pragma unroll
     for (int k = 0; k < 4 * kND; ++k) {
       const f32x4 x = left[64 * k];

@@ -212,6 +212,46 @@ def test_logits_that_run_away(d, hq, hkv):
         same(out, ref, size, most, d)
 
 
+# one prompt whose rows two groups of waves share: tiles of 64 keys in turns, each group with a reference of its own
+TWO_GROUPS = [(48, 24, 500), (24, 12, 900)]
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv,n", TWO_GROUPS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("top", [60, 100, 127, 200])
+@pytest.mark.parametrize("first,late", [(0, 100), (64, 140), (0, 239), (64, 300)])
+def test_references_of_two_groups_far_apart(d, hq, hkv, n, top, first, late):
+    """The first keys of one group lie 2^top above those of the other, which has a key of nearly that weight later on.  Logits are in powers
+    of two, in channel 0."""
+    gen = torch.Generator().manual_seed(n + top)
+    q, k, v = randn(gen, n, hq, d, scale=0.25), randn(gen, n, hkv, d, scale=0.25), randn(gen, n, hkv, d)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    k[first, :, 0], k[late, :, 0] = float(top), top - 0.5
+    v[first], v[late] = v[first] - 2.0, v[late] + 2.0
+    scale = math.log(2)
+    out = K.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), int32([0, n]), softmax_scale=scale)
+    torch.cuda.synchronize()
+    ref, size, most = causal(q, k, v, [0, n], scale)
+    same(out, ref, size, most, d)
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv,n", TWO_GROUPS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_that_run_away_in_two_groups(d, hq, hkv, n):
+    gen = torch.Generator().manual_seed(n + d)
+    for rows in (slice(250, 251), slice(40, n)):
+        q, k, v = randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)
+        q[rows] = (30 * q[rows].float()).to(torch.bfloat16)
+        k[200] = q[250, 0]
+        k[300:] = (10 * k[300:].float()).to(torch.bfloat16)
+        out = K.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), int32([0, n]))
+        torch.cuda.synchronize()
+        ref, size, most = causal(q, k, v, [0, n], d ** -0.5)
+        same(out, ref, size, most, d)
+
+
 @gpu
 @pytest.mark.parametrize("hq,hkv", [(2, 1), (96, 48), (48, 24)])
 @pytest.mark.parametrize("d", [64, 128])
