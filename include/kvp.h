@@ -482,7 +482,8 @@ int kvp_prompt_attention(const kvp_prompts* prompts, void* stream);
  * h / (n_q_heads / n_kv_heads), in fp32, rounded once; softmax_scale 0 means
  * 1/sqrt(head_dim).  Keys of a page whose number is not in 0 .. n_pages - 1 take no
  * part, whatever the pages hold behind a sequence's end neither; a sequence that is
- * left with no key has zeros for its result.  The same arguments give the same bits.
+ * left with no key has zeros for its result, and one with keys whose logits are all minus
+ * infinity NaNs (0 / 0), as from kvp_prompt_attention.  The same arguments give the same bits.
  * KVP_EINVAL also for more than 16 query heads per KV head, and where
  * n_seqs * n_kv_heads * table_width * page_size passes 2^38; KVP_ENOMEM for a
  * workspace that is too small. */

@@ -92,6 +92,11 @@ __device__ __forceinline__ bf16x8 lds_read_vt16(const unsigned char* p, int rows
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Logits that are all minus infinity leave a sum of 0, as no key does.  To tell 0 / 0 from a result of zeros the reference of a part with keys is never
+// less than the lowest number, beside which a sum of 0 is as good as beside minus infinity.
+constexpr float kLowest = -3.40282347e38f;
+__device__ __forceinline__ float inverse_of(float sum, float reference) { return sum == 0.f ? (reference == -INFINITY ? 0.f : NAN) : 1.f / sum; }
+
 // ---- where the units of the sequences begin, in all lanes of a wave
 __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, int seq) {
   return seq < a.n_seqs ? min(max(a.lengths[seq], 0), a.width << a.pool.shift) : 0;
@@ -266,6 +271,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
+    unsigned seen = 0;                             // bytes of keys that take part, or'ed (alone: block_bytes has all of them)
 
     struct Tile {
       unsigned long long at[2];          // its blocks in the pages
@@ -314,6 +320,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
     for (int t = t0; t < my_end; ++t) {
       const Tile now = next;
       const bool more = t + 1 < my_end;
+      if constexpr (!kDirect) seen |= now.bytes[0] | now.bytes[1];
       // ---- logits
       wait_all_but(VLoads{});
       f32x4 s[2];
@@ -409,6 +416,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       y = l;
       swap_lanes<32>(l, y);
       l += y;
+      if (kDirect ? __any(block_bytes != 0) : seen != 0) m = fmaxf(m, kLowest);
     }
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) reinterpret_cast<f32x4*>(k_strip)[64 * dt + lane] = o[dt];
@@ -436,14 +444,14 @@ paged_decode_kernel(const PagedDecodeArgs a) {
         sum += f[w] * reinterpret_cast<const f32x4*>(lds + w * S::kWaveBytes)[item];
       }
       if (whole) {
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const float inv = inverse_of(total, top);
         const u32x2 y = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
         *reinterpret_cast<u32x2*>(a.out + ((size_t)seq * a.n_q_heads + head * a.group + column) * D + ch) = y;
       } else {
         *reinterpret_cast<f32x4*>(a.partial + (slot + column) * D + ch) = sum;
         if (ch == 0) {
           float* const stat = a.partial + (size_t)2 * a.workgroups * a.group * D + 2 * (slot + column);
-          stat[0] = top * sl2;
+          stat[0] = top == kLowest ? kLowest : top * sl2;
           stat[1] = total;
         }
       }
@@ -531,7 +539,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedDec
     swap_lanes<32>(x, y);
     o[e] = x + y;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = inverse_of(l, m);
   if (sub == 0) reinterpret_cast<u32x2*>(out)[piece] = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
 }
 
@@ -601,7 +609,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_many_kernel(const Pag
   const int in_use = min((int)n, kSlots);
   f32x4 sum = rows[0][tid];
   for (int i = 1; i < in_use; ++i) sum += rows[i][tid];
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const float inv = inverse_of(total, top);
   reinterpret_cast<u32x2*>(out)[tid] = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 

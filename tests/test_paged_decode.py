@@ -326,3 +326,39 @@ def test_refusals_of_tensors():
         with pytest.raises(K.KvpError):
             pages.decode(**dict(good, **bad))
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("width", [16, 300])                                   # a workgroup for each sequence and head, and in shares
+@pytest.mark.parametrize("d,hq,hkv", [(128, 8, 2), (64, 5, 1)])
+def test_logits_of_minus_infinity(d, hq, hkv, width):
+    """Softmax of nothing but minus infinity is 0 / 0; beside a logit that is finite such keys weigh nothing; and without any key the result is zeros."""
+    gen = torch.Generator().manual_seed(d + width)
+    page, lengths = 64, [1000, 1000, 1000, 1000, 0, 40, 700]
+    pages, table = a_batch(gen, lengths, hkv, d, page, False)
+    table = torch.cat([table, torch.full((len(lengths), width - table.shape[1]), -1, dtype=torch.int32, device=DEV)], 1)
+    q = (torch.randn(len(lengths), hq, d, generator=gen).abs() + 0.125).to(torch.bfloat16)
+
+    def hide(seq, *keys):
+        for i in keys:
+            pages.k[table[seq, i // page].item(), :, i % page] = -math.inf
+
+    hide(0, *range(1000))                                                      # all
+    hide(1, *range(999))                                                       # all but the last one
+    hide(2, *range(1, 1000))                                                   # all but the first one
+    hide(3, *range(128, 600))
+    hide(5, *range(40))
+    hide(6, *range(700))
+    table[6] = -1                                                              # no key of these is there
+    out = pages.decode(q.to(DEV), table, int32(lengths), workspace=pages.workspace(hq).fill_(0xFF))
+    torch.cuda.synchronize()
+    assert torch.isnan(out[[0, 5]]).all() and not out[[4, 6]].any()
+    finite = pages.k.nan_to_num(neginf=0.0)
+    for s, seen in ((1, [999]), (2, [0]), (3, [*range(128), *range(600, 1000)])):
+        for h in range(hq):
+            at = [(table[s, i // page].item(), h // (hq // hkv), i % page) for i in seen]
+            k, v = (torch.stack([t[i] for i in at]).double().cpu() for t in (finite, pages.v))
+            one = q[s, h].double()
+            w = torch.softmax(k @ one * d ** -0.5, 0)
+            most = float((k.abs() @ one.abs()).max()) * d ** -0.5
+            check(out[s, h], (w @ v).numpy(), (w @ v.abs()).numpy(), most, d)
