@@ -362,3 +362,44 @@ def test_logits_of_minus_infinity(d, hq, hkv, width):
             w = torch.softmax(k @ one * d ** -0.5, 0)
             most = float((k.abs() @ one.abs()).max()) * d ** -0.5
             check(out[s, h], (w @ v).numpy(), (w @ v.abs()).numpy(), most, d)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (16, 8, 128)])
+@pytest.mark.parametrize("n,empty", [(64, 0), (65, 0), (64, 63), (128, 64), (129, 64), (129, -64), (200, 128), (300, -130)])
+def test_shares_of_more_sequences_than_a_wave_has_lanes(n, empty, hq, hkv, d, e4m3):
+    """Lengths are added up 64 at a time: groups of sequences that are empty before, behind and between others, under a table that says little."""
+    gen = torch.Generator().manual_seed(n + empty + d)
+    lengths = [int(x) for x in torch.randint(0, 700, (n,), generator=gen)]
+    begin = 0 if empty >= 0 else 70 if n > 200 else 32
+    lengths[begin:begin + abs(empty)] = [0] * abs(empty)
+    lengths[-1], lengths[n // 2 + 40 if n > 128 else -2] = 2900, 257
+    pages, table = a_batch(gen, lengths, hkv, d, 32, e4m3)
+    wide = torch.full((n, table.shape[1] + 30), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    q = torch.randn(n, hq, d, generator=gen).to(torch.bfloat16)
+    print("paged decode, many in shares", n, empty, hq, hkv, d, e4m3, flush=True)
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device=DEV)
+    pages.decode(q.to(DEV), wide, int32(lengths), out=out, workspace=pages.workspace(hq).fill_(0xFF))
+    torch.cuda.synchronize()
+    ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, 32, d ** -0.5)
+    check(out, ref, size, most, d)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("width", [2, 200])
+def test_as_many_sequences_as_a_call_takes(width, e4m3):
+    gen = torch.Generator().manual_seed(width)
+    n, hq, hkv, d, page = K.KVP_MAX_SEQUENCES, 2, 1, 64, 16
+    lengths = [int(x) for x in torch.randint(0, 33, (n,), generator=gen)]
+    lengths[100:500] = [0] * 400
+    pages, table = a_batch(gen, lengths, hkv, d, page, e4m3)
+    wide = torch.full((n, width), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    q = torch.randn(n, hq, d, generator=gen).to(torch.bfloat16)
+    out = pages.decode(q.to(DEV), wide, int32(lengths))
+    torch.cuda.synchronize()
+    ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, page, d ** -0.5)
+    check(out, ref, size, most, d)
