@@ -138,10 +138,12 @@ struct Numbers {                  // bf16 rows [tokens, heads, d]
   void* at;
   int64_t token, head;
 };
+// (An address may have to be made, and torch may throw for it: like all that looks at tensors these belong where exceptions are caught.)
+void* numbers_at(const at::Tensor* t) { return t->numel() > 0 ? t->mutable_data_ptr() : nullptr; }
 bool numbers(PyObject* o, int64_t device, int64_t tokens, int64_t heads, int64_t d, Numbers* out) {
   const at::Tensor* t;
   if (!plain_of(o, device, at::kBFloat16, &t) || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads || t->size(2) != d || t->stride(2) != 1) return false;
-  *out = Numbers{t->numel() > 0 ? t->mutable_data_ptr() : nullptr, tokens > 1 ? t->stride(0) : 0, heads > 1 ? t->stride(1) : 0};
+  *out = Numbers{numbers_at(t), tokens > 1 ? t->stride(0) : 0, heads > 1 ? t->stride(1) : 0};
   return true;
 }
 // contiguous int32 numbers
@@ -160,10 +162,10 @@ PyObject* page_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
       !small_int(args[4], &device) || !address(args[5], &stream))
     Py_RETURN_NONE;
   kvp_rows rows;
-  const at::Tensor *begin, *table, *first = nullptr;
+  const int32_t *begin_at, *table_at, *first_at = nullptr;
   int32_t n_seqs, width;
   try {
-    const at::Tensor* k;
+    const at::Tensor *k, *begin, *table, *first = nullptr;
     Numbers kn, vn;
     if (!plain_of(args[6], device, at::kBFloat16, &k) || k->dim() != 3 || k->size(0) > INT32_MAX) Py_RETURN_NONE;
     const int64_t n = k->size(0);
@@ -174,13 +176,16 @@ PyObject* page_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     rows = kvp_rows{kn.at, vn.at, kn.token, kn.head, vn.token, vn.head, (int32_t)n};
     n_seqs = (int32_t)table->size(0);
     width = (int32_t)table->size(1);
+    begin_at = ints(begin);
+    table_at = ints(table);
+    if (first) first_at = ints(first);
   } catch (...) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
   int code;
   Py_BEGIN_ALLOW_THREADS;
-  code = ((decltype(&kvp_page_write))entry)((const kvp_pages*)pages, &rows, ints(begin), ints(table), width, first ? ints(first) : nullptr, n_seqs, stream);
+  code = ((decltype(&kvp_page_write))entry)((const kvp_pages*)pages, &rows, begin_at, table_at, width, first_at, n_seqs, stream);
   Py_END_ALLOW_THREADS;
   return PyLong_FromLong(code);
 }
@@ -198,11 +203,14 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
       !small_int(args[4], &device) || !address(args[5], &stream) || !PyFloat_CheckExact(args[11]))
     Py_RETURN_NONE;
   const bool own = small_int(args[10], &bytes);
-  const at::Tensor *table, *lengths, *out, *room;
+  const int32_t *table_at, *lengths_at;
+  void *out_at, *room_at;
+  size_t room_bytes;
   at::Tensor made;
   Numbers q;
   int32_t n_seqs, width;
   try {
+    const at::Tensor *table, *lengths, *out, *room;
     if (!whole(args[7], device, &table) || !whole(args[8], device, &lengths) || table->dim() != 2 || lengths->dim() != 1) Py_RETURN_NONE;
     if (lengths->size(0) > INT32_MAX || table->size(0) != lengths->size(0) || table->size(1) > INT32_MAX) Py_RETURN_NONE;
     n_seqs = (int32_t)lengths->size(0);
@@ -215,6 +223,11 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     } else if (!plain_of(args[10], device, at::kByte, &room) || !room->is_contiguous()) {
       Py_RETURN_NONE;
     }
+    table_at = ints(table);
+    lengths_at = ints(lengths);
+    out_at = numbers_at(out);
+    room_at = numbers_at(room);
+    room_bytes = (size_t)room->numel();
   } catch (...) {
     PyErr_Clear();
     Py_RETURN_NONE;
@@ -222,9 +235,8 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   int code;
   const float scale = (float)PyFloat_AS_DOUBLE(args[11]);
   Py_BEGIN_ALLOW_THREADS;
-  code = ((decltype(&kvp_paged_decode))entry)((const kvp_pages*)pages, q.at, q.token, q.head, heads, ints(table), width, ints(lengths), n_seqs, scale,
-                                              out->numel() > 0 ? out->mutable_data_ptr() : nullptr,
-                                              room->numel() > 0 ? room->mutable_data_ptr() : nullptr, (size_t)room->numel(), stream);
+  code = ((decltype(&kvp_paged_decode))entry)((const kvp_pages*)pages, q.at, q.token, q.head, heads, table_at, width, lengths_at, n_seqs, scale, out_at, room_at,
+                                              room_bytes, stream);
   Py_END_ALLOW_THREADS;
   return PyLong_FromLong(code);
 }

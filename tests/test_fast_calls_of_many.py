@@ -3,6 +3,8 @@ only looks at its arguments."""
 import ctypes
 import importlib.util
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -116,3 +118,43 @@ def test_prompt(module):
                                (4, [k[1:], k[0], k.float(), wide[1], rows_of(3, 4, 64), None]), (5, [v[1:], v[:, 1:], v.float(), wide[1], None]),
                                (6, [None, begin.long(), begin[None], begin[:0], int32(0, 0, 1, 1, 3, 3)[::2]]),
                                (7, [out[1:], out[:, 1:], out.float(), wide[0], None]), (8, [None, 1, "1"])], taken)
+
+
+NO_ROOM = """
+import importlib.util, os, resource, sys
+sys.path.insert(0, %r)
+from tests import test_fast_calls_of_many as T
+spec = importlib.util.spec_from_file_location("_fast_calls", %r)
+module = importlib.util.module_from_spec(spec)
+spec.loader.exec_module(module)
+name, at, taken = %r, %d, []
+entry = {"page_rows": T.ROWS, "paged_decode": T.DECODE, "prompt": T.PROMPT}[name](lambda *args: taken.append(args) or 7)
+args = T.large(name, T.address(entry))
+whole = args[at]
+args[at] = T.torch._lazy_clone(whole)
+with open("/proc/self/statm") as f:
+    size = int(f.read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (size + (1 << 28), resource.RLIM_INFINITY))
+found = getattr(module, name)(*args)
+print("left" if found is None and not taken else (found, taken), flush=True)
+os._exit(0)          # (torch ends the process when it frees a clone that it could not copy)
+"""
+
+
+def large(name, entry):
+    """Arguments whose bf16 tensors and workspace have 1 GiB each, none of which is touched."""
+    new, begin, d = lambda *shape: torch.empty(*shape, dtype=BF16), int32(0, 1, 2), 1 << 27
+    if name == "page_rows":
+        return [entry, 11, 2, d, -1, 13, new(2, 2, d), new(2, 2, d), begin, torch.zeros(2, 6, dtype=torch.int32), int32(4, 5)]
+    if name == "paged_decode":
+        return [entry, 11, 2, d, -1, 13, new(2, 2, d), torch.zeros(2, 6, dtype=torch.int32), int32(1, 2), new(2, 2, d), torch.empty(1 << 30, dtype=torch.uint8), 0.25]
+    return [entry, -1, 13, new(2, 2, d), new(2, 2, d), new(2, 2, d), begin, new(2, 2, d), 0.5]
+
+
+@pytest.mark.parametrize("name,at", [("paged_decode", 9), ("paged_decode", 10), ("paged_decode", 6), ("page_rows", 6), ("page_rows", 7), ("prompt", 3), ("prompt", 7)])
+def test_tensors_that_have_to_be_copied_and_no_room_for_it(module, name, at):
+    """Torch copies a lazy clone when its address is asked for, and throws where it cannot: no exception may leave the module (a process of its
+    own, which it would end)."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", NO_ROOM % (root, module.__file__, name, at)], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and run.stdout.strip() == "left", (run.returncode, run.stderr[-500:])
