@@ -150,6 +150,19 @@ bool numbers(PyObject* o, int64_t device, int64_t tokens, int64_t heads, int64_t
 bool whole(PyObject* o, int64_t device, const at::Tensor** out) { return plain_of(o, device, at::kInt, out) && (*out)->is_contiguous(); }
 const int32_t* ints(const at::Tensor* t) { return t->numel() > 0 ? static_cast<const int32_t*>(t->const_data_ptr()) : nullptr; }
 
+// The kvp_pages, by its address or by (address, k, v, k_exp, v_exp): tensors, or None without exponents, whose memory has to be what it says.
+bool pages_of(PyObject* o, void** out) {
+  if (!PyTuple_CheckExact(o)) return address(o, out) && *out;
+  if (PyTuple_GET_SIZE(o) != 5 || !address(PyTuple_GET_ITEM(o, 0), out) || !*out) return false;
+  const kvp_pages& p = *static_cast<const kvp_pages*>(*out);
+  const void* const said[4] = {p.k, p.v, p.k_exp, p.v_exp};
+  for (int i = 0; i < 4; ++i) {
+    PyObject* const t = PyTuple_GET_ITEM(o, i + 1);
+    if (t == Py_None ? said[i] != nullptr : !THPVariable_Check(t) || THPVariable_Unpack(t).const_data_ptr() != said[i]) return false;
+  }
+  return true;
+}
+
 // page_rows(entry, pages, n_kv_heads, head_dim, device, stream, k, v, seq_begin, table, first)
 PyObject* page_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   if (n_args != 11) {
@@ -158,13 +171,14 @@ PyObject* page_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
   void *entry, *pages, *stream;
   int32_t heads, d, device;
-  if (!address(args[0], &entry) || !entry || !address(args[1], &pages) || !pages || !small_int(args[2], &heads) || !small_int(args[3], &d) ||
-      !small_int(args[4], &device) || !address(args[5], &stream))
+  if (!address(args[0], &entry) || !entry || !small_int(args[2], &heads) || !small_int(args[3], &d) || !small_int(args[4], &device) ||
+      !address(args[5], &stream))
     Py_RETURN_NONE;
   kvp_rows rows;
   const int32_t *begin_at, *table_at, *first_at = nullptr;
   int32_t n_seqs, width;
   try {
+    if (!pages_of(args[1], &pages)) Py_RETURN_NONE;
     const at::Tensor *k, *begin, *table, *first = nullptr;
     Numbers kn, vn;
     if (!plain_of(args[6], device, at::kBFloat16, &k) || k->dim() != 3 || k->size(0) > INT32_MAX) Py_RETURN_NONE;
@@ -199,8 +213,8 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
   void *entry, *pages, *stream;
   int32_t heads, d, device, bytes = 0;
-  if (!address(args[0], &entry) || !entry || !address(args[1], &pages) || !pages || !small_int(args[2], &heads) || !small_int(args[3], &d) ||
-      !small_int(args[4], &device) || !address(args[5], &stream) || !PyFloat_CheckExact(args[11]))
+  if (!address(args[0], &entry) || !entry || !small_int(args[2], &heads) || !small_int(args[3], &d) || !small_int(args[4], &device) ||
+      !address(args[5], &stream) || !PyFloat_CheckExact(args[11]))
     Py_RETURN_NONE;
   const bool own = small_int(args[10], &bytes);
   const int32_t *table_at, *lengths_at;
@@ -210,6 +224,7 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   Numbers q;
   int32_t n_seqs, width;
   try {
+    if (!pages_of(args[1], &pages)) Py_RETURN_NONE;
     const at::Tensor *table, *lengths, *out, *room;
     if (!whole(args[7], device, &table) || !whole(args[8], device, &lengths) || table->dim() != 2 || lengths->dim() != 1) Py_RETURN_NONE;
     if (lengths->size(0) > INT32_MAX || table->size(0) != lengths->size(0) || table->size(1) > INT32_MAX) Py_RETURN_NONE;

@@ -96,7 +96,19 @@ def prompt_attention(q, k, v, seq_begin, out=None, softmax_scale=0.0, stream=Non
 
 class Pages:
     """Pages of one layer over the caller's tensors, [n_pages, n_kv_heads, page_size, head_dim]: `k` and `v` of bf16, or of e4m3
-    (torch.float8_e4m3fn) with exponents `k_exp` and `v_exp`, uint8 [n_pages, n_kv_heads, page_size]."""
+    (torch.float8_e4m3fn) with exponents `k_exp` and `v_exp`, uint8 [n_pages, n_kv_heads, page_size].  The tensors are kept, and cannot be
+    exchanged; a call after one of them has been given other memory (resize_, set_) is refused."""
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_exp = property(lambda self: self._tensors[2])
+    v_exp = property(lambda self: self._tensors[3])
+    device = property(lambda self: self._device)
+    n_pages = property(lambda self: self._shape[0])
+    n_kv_heads = property(lambda self: self._shape[1])
+    page_size = property(lambda self: self._shape[2])
+    head_dim = property(lambda self: self._shape[3])
+    of = property(lambda self: KvpPages.from_buffer_copy(self._of), doc="For the calls of include/kvp.h, a copy.")
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         import torch
@@ -109,15 +121,14 @@ class Pages:
             _need((t is not None) == e4m3, "Pages: exponents belong to e4m3")
             if t is not None:
                 _need(t.shape == k.shape[:3] and t.dtype is torch.uint8 and t.device == k.device and t.is_contiguous(), "Pages: exponents")
-        self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        self.of = KvpPages(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if e4m3 else None, v_exp.data_ptr() if e4m3 else None,
-                           KVP_PAGE_E4M3 if e4m3 else KVP_PAGE_BF16, *k.shape)
-        self._ref, self._lib = ctypes.byref(self.of), lib()
+        self._tensors, self._device, self._shape = (k, v, k_exp, v_exp), k.device, tuple(k.shape)
+        self._of = KvpPages(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if e4m3 else None, v_exp.data_ptr() if e4m3 else None,
+                            KVP_PAGE_E4M3 if e4m3 else KVP_PAGE_BF16, *k.shape)
+        self._ref, self._lib = ctypes.byref(self._of), lib()
         # what every call needs, looked up once (rows of a few sequences take the GPU 2.6 us; through Python alone a call took the host 8)
         native = _fast_call("page_rows"), _fast_call("paged_decode")
         device, stream, index = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, k.device.index
-        at, heads, dim, work = ctypes.addressof(self.of), self.n_kv_heads, self.head_dim, {}
+        at, heads, dim, work = (ctypes.addressof(self._of), *self._tensors), k.shape[1], k.shape[3], {}
         rows, decode, write_entry, read_entry, decode_entry = *native, _entries.kvp_page_write, _entries.kvp_page_read, _entries.kvp_paged_decode
         self._work = work
 
@@ -145,7 +156,14 @@ class Pages:
             return cls(new(shape, torch.bfloat16), new(shape, torch.bfloat16))
         return cls(new(shape, torch.float8_e4m3fn), new(shape, torch.float8_e4m3fn), new(shape[:3], torch.uint8), new(shape[:3], torch.uint8))
 
+    def _need_memory(self):
+        """The tensors' memory is where it was when its addresses were taken.  (The native calls look for themselves.)"""
+        of = self._of
+        for t, at in zip(self._tensors, (of.k, of.v, of.k_exp, of.v_exp)):
+            _need(t is None or t.data_ptr() == at, "Pages: a tensor has other memory than it had")
+
     def _rows(self, call, k, v, seq_begin, table, first, stream):
+        self._need_memory()
         n_tokens, n_seqs, device = k.shape[0], seq_begin.numel() - 1, self.device
         what = "Pages.%s: " % call
         shape = (n_tokens, self.n_kv_heads, self.head_dim)
@@ -202,6 +220,7 @@ class Pages:
                 return out
             if rc is not None:
                 raise KvpError(rc, "kvp_paged_decode")
+        self._need_memory()
         n_seqs, device = lengths.numel(), self.device
         _need(q.dim() == 3 and table.dim() == 2, "Pages.decode: q and table")
         n_q_heads, what = q.shape[1], "Pages.decode: "

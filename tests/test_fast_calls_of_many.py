@@ -158,3 +158,33 @@ def test_tensors_that_have_to_be_copied_and_no_room_for_it(module, name, at):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     run = subprocess.run([sys.executable, "-c", NO_ROOM % (root, module.__file__, name, at)], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and run.stdout.strip() == "left", (run.returncode, run.stderr[-500:])
+
+
+@pytest.mark.parametrize("name", ["page_rows", "paged_decode"])
+def test_memory_of_the_pages(module, name):
+    """Pages by their tensors: taken while the tensors' memory is what the struct says, and left when one has been given other memory."""
+    taken = []
+    entry = {"page_rows": ROWS, "paged_decode": DECODE}[name](lambda *args: taken.append(args[0]) or 7)
+    if name == "page_rows":
+        rest = [2, 128, -1, 13, rows_of(3, 2, 128), rows_of(3, 2, 128), int32(0, 1, 3), torch.zeros(2, 6, dtype=torch.int32), None]
+    else:
+        rest = [4, 128, -1, 13, rows_of(2, 4, 128), torch.zeros(2, 6, dtype=torch.int32), int32(1, 2), rows_of(2, 4, 128), 4096, 0.25]
+    call = lambda pages: getattr(module, name)(address(entry), pages, *rest)
+    for n in (2, 4):
+        new = lambda: [torch.zeros(4, 2, 16, 64, dtype=torch.uint8) for _ in range(2)] + [torch.zeros(4, 2, 16, dtype=torch.uint8) if n == 4 else None for _ in range(2)]
+        tensors = new()
+        of = K.KvpPages(*(t.data_ptr() if t is not None else None for t in tensors), 1 if n == 4 else 0, 4, 2, 16, 64)
+        at = ctypes.addressof(of)
+        assert call((at, *tensors)) == 7 and taken.pop() == at
+        assert call(at) == 7 and taken.pop() == at
+        for bad in [(at, *tensors[:3]), (at, *tensors, None), (at, *tensors[1::-1], *tensors[2:]), (0, *tensors), (None, *tensors), [at, *tensors], (at, 1, *tensors[1:]),
+                    (at, *new()), (at, None, *tensors[1:]), (at, *tensors[:2], tensors[0], tensors[3])]:
+            assert call(bad) is None and not taken
+        for i in range(n):
+            for other in (lambda t: t.resize_(1 << 20), lambda t: t.set_(torch.zeros_like(t)), lambda t: setattr(t, "data", torch.zeros_like(t)),
+                          lambda t: t.untyped_storage().resize_(1 << 22)):
+                tensors = new()
+                of.k, of.v, of.k_exp, of.v_exp = (t.data_ptr() if t is not None else None for t in tensors)
+                assert call((at, *tensors)) == 7 and taken.pop() == at
+                other(tensors[i])
+                assert call((at, *tensors)) is None and not taken, i

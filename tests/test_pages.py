@@ -335,3 +335,38 @@ def test_refusals_of_tensors():
         K.Pages(row(4, 2, 64, 128), row(4, 2, 64, 128), torch.zeros(4, 2, 64, dtype=torch.uint8, device=DEV))
     with pytest.raises(K.KvpError):
         K.Pages(row(4, 2, 64, 128), row(4, 2, 64, 128).transpose(0, 1).contiguous().transpose(0, 1))
+
+
+def test_tensors_of_pages_cannot_be_exchanged():
+    for name in ("k", "v", "k_exp", "v_exp", "device", "n_pages", "n_kv_heads", "page_size", "head_dim", "of"):
+        found = getattr(K.Pages, name)
+        assert isinstance(found, property) and found.fset is None, name
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("native", [True, False])
+def test_pages_whose_memory_is_another_one(e4m3, native):
+    """The calls have the tensors' addresses: after resize_ or set_ these would be those of memory that is not theirs any more."""
+    row = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16, device=DEV)
+    stream = None if native else torch.cuda.current_stream()
+    args = dict(seq_begin=int32([0, 1, 3]), table=int32([[0], [1]]), stream=stream)
+    for name in ("k", "v", "k_exp", "v_exp")[:4 if e4m3 else 2]:
+        for change in (lambda t: t.resize_(2 * t.numel()), lambda t: t.set_(torch.zeros_like(t))):
+            pages = K.Pages.empty(4, 2, 128, 64, e4m3, DEV)
+            k, v, q, out = row(3, 2, 128), row(3, 2, 128), row(2, 4, 128), row(2, 4, 128)
+            calls = [lambda: pages.write(k, v, **args), lambda: pages.read(k, v, **args),
+                     lambda: pages.decode(q, args["table"], int32([1, 2]), out=out, stream=stream), lambda: pages.decode(q, args["table"], int32([1, 2]), stream=stream)]
+            for call in calls:
+                call()
+            with pytest.raises(AttributeError):
+                setattr(pages, name, torch.zeros_like(getattr(pages, name)))
+            pages.of.head_dim = 64                                              # of a copy
+            for call in calls:
+                call()
+            torch.cuda.synchronize()
+            change(getattr(pages, name))
+            for call in calls:
+                with pytest.raises(K.KvpError):
+                    call()
+    torch.cuda.synchronize()
