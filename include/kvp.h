@@ -378,6 +378,7 @@ void kvp_free_cache(kvp_cache* cache);   /* host object only; NULL is fine */
  * range is brought into it as each call says, and nothing outside the caller's
  * tensors is read or written for it.
  *
+ * A softmax_scale is not negative, and finite when multiplied by log2(e).
  * Device tensors of bf16 numbers start at a multiple of 16 bytes; strides are in
  * elements, multiples of 8 and not negative, those from token to token below 2^23 and
  * those from head to head below 2^40.  Rows of a tensor that is written do not overlap.

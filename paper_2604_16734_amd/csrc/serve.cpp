@@ -84,8 +84,8 @@ int prepared() {
 }
 
 bool valid_group(int32_t n_q_heads, int32_t n_kv_heads) { return n_q_heads >= 1 && n_kv_heads >= 1 && n_q_heads % n_kv_heads == 0; }
-bool valid_scale(float s) { return s >= 0.f && !std::isinf(s); }
 float scale_log2_of(float scale, int head_dim) { return (scale > 0.f ? scale : 1.f / std::sqrt((float)head_dim)) * 1.4426950408889634f; }
+bool valid_scale(float s) { return s >= 0.f && std::isfinite(scale_log2_of(s, 64)); }      // (what the kernels multiply by)
 
 }  // namespace
 

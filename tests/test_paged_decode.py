@@ -403,3 +403,12 @@ def test_as_many_sequences_as_a_call_takes(width, e4m3):
     torch.cuda.synchronize()
     ref, size, most = reference(q.double().numpy(), Pool(pages), table.cpu().numpy(), lengths, pages.n_pages, page, d ** -0.5)
     check(out, ref, size, most, d)
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_scales_that_are_too_large(scale):
+    """A scale is taken times log2(e), which these are not finite with: every result would be NaN."""
+    assert _decode(softmax_scale=scale) == K.KVP_EINVAL
+    prompts = K.KvpPrompts(q=P16, k=P16, v=P16, out=P16, seq_begin=P4, q_token=512, q_head=128, k_token=256, k_head=128, v_token=256, v_head=128, out_token=512,
+                           out_head=128, n_tokens=5, n_seqs=2, n_q_heads=4, n_kv_heads=2, head_dim=128, softmax_scale=scale)
+    assert K.kvp_prompt_attention(prompts) == K.KVP_EINVAL
