@@ -370,3 +370,31 @@ def test_pages_whose_memory_is_another_one(e4m3, native):
                 with pytest.raises(K.KvpError):
                     call()
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_as_many_sequences_as_a_call_takes(e4m3):
+    gen = torch.Generator().manual_seed(21)
+    n_seqs, heads, d, page, width = K.KVP_MAX_SEQUENCES, 3, 64, 16, 2
+    lengths = [int(x) for x in torch.randint(0, 4, (n_seqs,), generator=gen)]
+    lengths[200:600] = [0] * 400
+    begin = np.concatenate([[0], np.cumsum(lengths)]).astype(int) + 5
+    first = [int(x) for x in torch.randint(0, 28, (n_seqs,), generator=gen)]
+    n, n_pages = int(begin[-1]) + 2, n_seqs * width
+    table = torch.randperm(n_pages, generator=gen).view(n_seqs, width).int()
+    pages = a_pool(gen, n_pages, heads, d, page, e4m3)
+    expected = Pool(pages)
+    k, v = numbers(gen, n, heads, d), numbers(gen, n, heads, d)
+    args = (int32(begin.tolist()), table.to(DEV), int32(first))
+    pages.write(k.to(DEV), v.to(DEV), *args)
+    k_ref, v_ref = np.full(k.shape, 3.0), np.full(v.shape, 3.0)
+    for t, number, offset in placed(begin, first, table, n_pages, page, n):
+        expected.put("k", number, offset, k[t].double().numpy())
+        expected.put("v", number, offset, v[t].double().numpy())
+        for h in range(heads):
+            k_ref[t, h], v_ref[t, h] = expected.row("k", number, h, offset), expected.row("v", number, h, offset)
+    assert expected.same(pages)
+    kr, vr = torch.full_like(k, 3.0).to(DEV), torch.full_like(v, 3.0).to(DEV)
+    pages.read(kr, vr, *args)
+    assert np.array_equal(kr.double().cpu().numpy(), k_ref) and np.array_equal(vr.double().cpu().numpy(), v_ref)

@@ -400,3 +400,39 @@ def test_prompts_pages_and_steps_together(e4m3):
     assert other.decode_ready(0)[4] == budget
     torch.cuda.synchronize()
     cache.close(), other.close()
+
+
+@gpu
+@pytest.mark.parametrize("n,hq,hkv", [(450, 4, 2), (450, 96, 48), (900, 24, 12)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_far_before_a_number_that_is_not_finite_have_the_same_bits(d, n, hq, hkv):
+    """Rows of the 64 that such a key is among may be taken again, with weights that are not rounded; those before them are not, nor other prompts, nor
+    heads that read another KV head."""
+    gen = torch.Generator().manual_seed(d + n)
+    q, k, v = (x.to(DEV) for x in (randn(gen, n, hq, d), randn(gen, n, hkv, d), randn(gen, n, hkv, d)))
+    begin = int32([0, 100, n])
+    good = K.prompt_attention(q, k, v, begin)
+    for row, upto in ((70, 64), (100 + 130, 100 + 128), (n - 1, n - 1 - (n - 101) % 64)):
+        k2, v2 = k.clone(), v.clone()
+        k2[row, 0, 3], v2[row, 0, 5] = math.nan, math.inf
+        out = K.prompt_attention(q, k2, v2, begin)
+        torch.cuda.synchronize()
+        same_bits = torch.ones(n, hq, dtype=torch.bool, device=DEV)
+        same_bits[upto:100 if row < 100 else n, :hq // hkv] = False
+        assert torch.equal(out[same_bits], good[same_bits]) and not torch.isfinite(out[row, :hq // hkv]).all()
+
+
+@gpu
+@pytest.mark.parametrize("lengths", [(0, 3), (20, 70)])
+def test_as_many_prompts_as_a_call_takes(lengths):
+    gen = torch.Generator().manual_seed(lengths[1])
+    lengths = [int(x) for x in torch.randint(*lengths, (K.KVP_MAX_SEQUENCES,), generator=gen)]
+    lengths[1000:1300] = [0] * 300
+    begin = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    n = begin[-1]
+    q, k, v = randn(gen, n, 2, 64), randn(gen, n, 1, 64), randn(gen, n, 1, 64)
+    out = K.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), int32(begin))
+    torch.cuda.synchronize()
+    ref, size, most = causal(q, k, v, begin, 0.125)
+    assert np.isfinite(ref).all()
+    same(out, ref, size, most, 64)
