@@ -1,7 +1,7 @@
 // One decode step of many sequences, each over its own pages (kvp_paged_decode): out = softmax(scale q K^T) V with one query row per
 // query head.
 //
-// Bound by HBM (96 sequences of up to 16640 keys, 32/8 heads, d 128, bf16: 313 us, 5.75 TB/s, what a copy reaches): every key and value is read once
+// Bound by HBM (96 sequences of up to 16640 keys, 12 of them without any, 32/8 heads, d 128, bf16: 314 us, 5.7 TB/s, what a copy reaches): every key and value is read once
 // and meets the G query heads of its KV head, 4 G flops for two numbers.  So what counts is
 // that every CU has loads on their way all the time, and that none of them has more to do than the others.
 //
@@ -18,8 +18,8 @@
 // Products.  S^T = K Q^T with 16x16x32 matrix instructions: rows are 16 keys, columns the query heads of the KV head (up to 16; the columns
 // beyond repeat the last one and are dropped).  A lane has four neighbouring keys of one query head of each 16, and these eight exponentials are, as they lie, its
 // part of the second operand of O^T = V^T P^T, whose first comes out of LDS by transposing reads in the same order of keys.  e4m3 numbers
-// become bf16 on the way from LDS to the matrix instruction, exactly; the powers of two of the rows are applied to the logits (K) and to the
-// weights (V), exactly, too.  Sums and maxima are in fp32; weights are rounded to bf16 for the product only.
+// become bf16 on the way from LDS to the matrix instruction, exactly; the powers of two of the rows are applied to the keys and to the
+// weights (V), exactly, too, but for weights that come out below 2^-126, the least bf16 number of full precision.  Sums and maxima are in fp32; weights are rounded to bf16 for the product only.
 #include <type_traits>
 
 #include "mfma_tools.h"
@@ -315,7 +315,7 @@ paged_decode_kernel(const PagedDecodeArgs a) {
       issue_k(next);
       issue_v(next);
 #pragma unroll
-      for (int st = 0; st < kSteps; ++st) asm volatile("" : "+v"(qf[st]));         // (as page_rows)
+      for (int st = 0; st < kSteps; ++st) asm volatile("" : "+v"(qf[st]));         // here, as block_at
     }
     for (int t = t0; t < my_end; ++t) {
       const Tile now = next;

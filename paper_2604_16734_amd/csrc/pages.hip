@@ -8,8 +8,9 @@
 // those nearest to the input whose exponent allows four significant bits.  The way back is exact, too: a bf16 number of which four
 // significant bits are left is still one (a multiple of 2^-133, and only what rounds up to 2^128 is none).
 //
-// Bound by HBM: the bf16 side is read or written once, the pages once (12 sequences of 32 heads, d 64, out of bf16 pages of 16: 146 us, 5.2 TB/s), and by
-// latency where there are few (1024 tokens of 4 heads out of e4m3 pages 3.1 us).
+// Bound by HBM: the bf16 side is read or written once, the pages once (11 sequences of 32 heads, d 64, out of bf16 pages of 16: 147 us, 5.2 TB/s), and by
+// latency where there are few (1024 tokens of 4 heads out of e4m3 pages 3.2 us).  bf16 into pages, four rows a wave, is not there yet: the compiler keeps three of the rows of K
+// in scratch memory (17976 tokens of 8 heads, d 128, 41 us for 147 MB).
 #include <type_traits>
 
 #include "lane_tools.h"
@@ -21,7 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // A wave has kUnits times the rows that its lanes hold at once, for the price of one search for their places: 4, or 1 where all waves
-// run at once anyway.  (20 K tokens of 8 heads, d 128, to e4m3 25.4 us with 1 and a search for every row, 20.4 with 4; 48 tokens 3.4 and 4.2 us.)
+// run at once anyway.  (17976 tokens of 8 heads, d 128, to e4m3 25.4 us with 1 and a search for every row, 20.4 with 4; 48 tokens 3.4 and 4.2 us.)
 
 // Where the first head's row of a token is in the pages: lane i's of token from + i.  The token's sequence is the number of those that begin no
 // later, less one; -1 or n_seqs: none.  One load and a vote per token for every 64 sequences.  What is needed of the sequence itself, where it begins and
