@@ -378,7 +378,11 @@ void kvp_free_cache(kvp_cache* cache);   /* host object only; NULL is fine */
  * range is brought into it as each call says, and nothing outside the caller's
  * tensors is read or written for it.
  *
- * A softmax_scale is not negative, and finite when multiplied by log2(e).
+ * Attention: a softmax_scale is not negative, and finite when multiplied by log2(e).
+ * Sums are in fp32; a softmax weight enters its product with V as a bf16 number, and the
+ * sum over the keys is divided by the sum of the weights at the end: it overflows where
+ * values times their number pass 3.4e38.
+ *
  * Device tensors of bf16 numbers start at a multiple of 16 bytes; strides are in
  * elements, multiples of 8 and not negative, those from token to token below 2^23 and
  * those from head to head below 2^40.  Rows of a tensor that is written do not overlap.
@@ -448,9 +452,10 @@ int kvp_page_read(const kvp_pages* pages, const kvp_rows* rows, const int32_t* s
  *   seq_begin device [n_seqs + 1], not descending, from 0 to n_tokens at most (brought
  *             into that range); rows of out that belong to no prompt are left as they were
  * Query head h reads KV head h / (n_q_heads / n_kv_heads).  fp32 accumulation, rounded
- * once; softmax_scale 0 means 1/sqrt(head_dim).  What a row does not see does not enter into
- * it, were it infinite; but up to 64 rows before a number that is not finite may be rounded otherwise
- * than without it (and 32 rows at a time take many times longer).  n_tokens = 0 does nothing.  KVP_EINVAL also where
+ * once; softmax_scale 0 means 1/sqrt(head_dim).  What a row does not see does not enter
+ * into it, were it infinite; but up to 63 rows before a number that is not finite may be
+ * rounded otherwise than without it, as their weights are then not rounded to bf16 (which
+ * takes many times longer).  n_tokens = 0 does nothing.  KVP_EINVAL also where
  * (n_tokens / 32 + n_seqs) * n_q_heads passes 2^30 - 64, or rows from token to token are
  * less than head_dim apart. */
 typedef struct kvp_prompts {
@@ -482,13 +487,13 @@ int kvp_prompt_attention(const kvp_prompts* prompts, void* stream);
  *              overlap in time need one each.
  * out[s, h] = softmax(scale * q[s, h] . K^T) V over the keys of KV head
  * h / (n_q_heads / n_kv_heads), in fp32, rounded once; softmax_scale 0 means
- * 1/sqrt(head_dim).  A softmax weight enters its product with V as a bf16 number, with
- * KVP_PAGE_E4M3 after the power of two of the value's row: below 2^-126 it has fewer bits,
- * so rows of values below about 2^-100 are not held to the precision of others.  Keys of a page whose number is not in 0 .. n_pages - 1 take no
- * part, whatever the pages hold behind a sequence's end neither; a sequence that is
- * left with no key has zeros for its result, and one with keys whose logits are all minus
- * infinity NaNs (0 / 0), as from kvp_prompt_attention.  The same arguments give the same bits.
- * KVP_EINVAL also for more than 16 query heads per KV head, and where
+ * 1/sqrt(head_dim).  With KVP_PAGE_E4M3 a weight is rounded to bf16 after the power of two
+ * of its value's row: below 2^-126 it has fewer bits, so that rows of values below about
+ * 2^-100 are not held to the precision of others.  Keys of a page whose number is not in
+ * 0 .. n_pages - 1 take no part, whatever the pages hold behind a sequence's end neither; a
+ * sequence that is left with no key has zeros for its result, and one with keys whose
+ * logits are all minus infinity NaNs (0 / 0), as from kvp_prompt_attention.  The same
+ * arguments give the same bits.  KVP_EINVAL also for more than 16 query heads per KV head, and where
  * n_seqs * n_kv_heads * table_width * page_size passes 2^38; KVP_ENOMEM for a
  * workspace that is too small. */
 size_t kvp_paged_decode_bytes(const kvp_pages* pages, int32_t n_q_heads);
