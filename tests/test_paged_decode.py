@@ -330,7 +330,7 @@ def test_refusals_of_tensors():
 
 @gpu
 @pytest.mark.parametrize("width", [16, 300])                                   # a workgroup for each sequence and head, and in shares
-@pytest.mark.parametrize("d,hq,hkv", [(128, 8, 2), (64, 5, 1)])
+@pytest.mark.parametrize("d,hq,hkv", [(128, 8, 2), (64, 5, 1), (128, 32, 8), (64, 48, 4)])      # (the last two: joins of many sequences)
 def test_logits_of_minus_infinity(d, hq, hkv, width):
     """Softmax of nothing but minus infinity is 0 / 0; beside a logit that is finite such keys weigh nothing; and without any key the result is zeros."""
     gen = torch.Generator().manual_seed(d + width)
